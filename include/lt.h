@@ -433,6 +433,134 @@ lt_status lt_rope_table(float* CS, int S, int D, double base,
 lt_status lt_rope_f16(lt_half* X, int64_t row_stride, int B, int S, int heads,
                       int D, const float* CS, int inverse, lt_stream stream);
 
+/*
+ * ---- Packed sequences: several documents laid end to end in one sequence ----
+ *
+ * Attention with modified scores (forward).  lt_attn_fwd's attention with, per
+ * batch row b, an interval of keys for every query, and optionally a cap and a
+ * distance bias on the scores:
+ *
+ *     s_ij  = scale * q_i . k_j
+ *     s_ij  = cap * tanh(s_ij / cap)          if cap > 0
+ *     s_ij -= slopes[h] * |i - j|             if slopes is given (h: query head)
+ *     query i sees the keys LO[b][i] <= j < HI[b][i], and of those only j <= i
+ *     when causal
+ *     P = row softmax over the keys seen, O_i = sum_j P_ij v_j,
+ *     LSE_i = ln sum_j exp(s_ij)
+ *
+ *   LO, HI: [B, S] int32 device arrays or NULL (LO: 0, HI: S); values are
+ *   clamped to 0 .. S.  Packed documents: LO = the document's start, causal = 1.  A
+ *   prefix mask: causal = 0, HI = max(i + 1, end of the prefix).  A sliding window:
+ *   LO = i - width + 1, causal = 1.  A padded batch: HI = the row's length, and
+ *   HI = 0 for the padding.  A query that sees no key gets O = 0 and LSE = -inf.
+ *   slopes: [Hq] FP32 device array or NULL.  cap: 0 for none, else up to 1000.
+ *   Layouts, head grouping and errors as lt_attn_fwd, and
+ *   LT_ERR_INVALID_ARG for a cap that is negative or not finite;
+ *   LT_ERR_UNSUPPORTED for cap > 1000, S > 2^19, or LO, HI, slopes not 4-byte
+ *   aligned.
+ */
+lt_status lt_attn_mod_fwd(const lt_half* Q, const lt_half* K, const lt_half* V,
+                          int64_t q_row_stride, int64_t kv_row_stride,
+                          lt_half* O, int64_t o_row_stride, float* LSE,
+                          const int32_t* LO, const int32_t* HI,
+                          const float* slopes, float cap, int B, int S, int Hq,
+                          int Hkv, int D, float scale, int causal,
+                          lt_stream stream);
+
+/*
+ * Its backward: with t = tanh(scale q.k / cap) (0 without a cap),
+ *     dP = dO V^T,  dS = P (dP - D) (1 - t^2),  D_i = rowsum(dO_i * O_i)
+ *     dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+ *   summed over the query heads of a key/value head; slopes are constants.  A
+ *   query that sees no key gets dQ = 0, a key that no query sees dK = dV = 0.
+ *   LO, HI, slopes, cap, scale and causal as given to the forward, O and LSE as
+ *   it wrote them.  dS is kept in FP16 between the passes, as in lt_attn_bwd,
+ *   for part of the (batch, key/value head) pairs at a time (about 4 GiB, or
+ *   one pair's if that is more).  Errors as the forward and lt_attn_bwd; the
+ *   workspace (256-byte aligned) needs lt_attn_mod_bwd_workspace_size bytes, 0
+ *   for invalid sizes.
+ */
+size_t lt_attn_mod_bwd_workspace_size(int B, int S, int Hq, int Hkv, int D,
+                                      int causal);
+lt_status lt_attn_mod_bwd(const lt_half* Q, const lt_half* K, const lt_half* V,
+                          int64_t q_row_stride, int64_t kv_row_stride,
+                          const lt_half* O, const lt_half* dO,
+                          int64_t o_row_stride, const float* LSE,
+                          const int32_t* LO, const int32_t* HI,
+                          const float* slopes, float cap, lt_half* dQ,
+                          lt_half* dK, lt_half* dV, int64_t dq_row_stride,
+                          int64_t dkv_row_stride, void* workspace,
+                          size_t ws_bytes, int B, int S, int Hq, int Hkv, int D,
+                          float scale, int causal, lt_stream stream);
+
+/*
+ * RMSNorm of every query and key head and the rotary embedding in one pass.
+ * Per token t = b*S + p and head h < Hq + Hkv (Q heads, then K heads, as in the
+ * fused QKV buffer), x = X[t, h*D .. h*D + D - 1]:
+ *     u = w x r,  r = (mean x^2 + eps)^(-1/2),  w = Wq (h < Hq) or Wk
+ *     y = u rotated as by lt_rope_f16, by the angles of table row POS[t]
+ *   CS: lt_rope_table's [P][D/2][2].  POS: [B*S] int32 device array of positions
+ *   (a document's restart at 0), NULL for p; a position outside 0 .. P - 1
+ *   writes NaN.  Y [T, >= (Hq + Hkv) D] with row stride ldy may be X itself
+ *   (ldy = ldx) where no backward follows.  RSTD [T, Hq + Hkv] FP32: r, kept for
+ *   the backward.  FP32 math, one rounding per output.
+ *   Errors: LT_ERR_INVALID_ARG for NULL pointers, sizes < 1, strides below
+ *   (Hq + Hkv) D, POS NULL with S > P, eps negative or not finite;
+ *   LT_ERR_UNSUPPORTED for D not a multiple of 16 or above 256, misaligned
+ *   pointers (16 bytes; POS, RSTD 4) or strides.
+ */
+lt_status lt_qknorm_rope_fwd(const lt_half* X, int64_t ldx, const lt_half* Wq,
+                             const lt_half* Wk, const float* CS, int P,
+                             const int32_t* POS, lt_half* Y, int64_t ldy,
+                             float* RSTD, int B, int S, int Hq, int Hkv, int D,
+                             float eps, lt_stream stream);
+
+/*
+ * Its backward, given dY and the forward's X and RSTD: g = dY rotated back,
+ *     dX = r w g - r^3 x mean(g w x),
+ *     dWq, dWk [D] = sums of g x r over tokens and query / key heads (FP16,
+ *     summed in FP32 in a fixed order: deterministic).
+ * dX may be dY itself (lddx = lddy).  The workspace (256-byte aligned) needs
+ * lt_qknorm_rope_bwd_workspace_size bytes, 0 for invalid sizes.  Errors as the
+ * forward, and LT_ERR_WORKSPACE.
+ */
+size_t lt_qknorm_rope_bwd_workspace_size(int B, int S, int Hq, int Hkv, int D);
+lt_status lt_qknorm_rope_bwd(const lt_half* dY, int64_t lddy, const lt_half* X,
+                             int64_t ldx, const lt_half* Wq, const lt_half* Wk,
+                             const float* RSTD, const float* CS, int P,
+                             const int32_t* POS, lt_half* dX, int64_t lddx,
+                             lt_half* dWq, lt_half* dWk, void* workspace,
+                             size_t ws_bytes, int B, int S, int Hq, int Hkv,
+                             int D, lt_stream stream);
+
+/*
+ * Token embedding with scaling: Y[t] = scale * W[ids[t]] for t < T, W [V, H]
+ * (row stride ldw), Y [T, H] (ldy), ids [T] int64 on the device.  An id outside
+ * 0 .. V - 1 (-1, say) is padding: a row of zeros.  One rounding per output.
+ * T == 0 is a no-op.  Errors: LT_ERR_INVALID_ARG for NULL pointers, T < 0, H or
+ * V < 1, strides below H, scale not finite; LT_ERR_UNSUPPORTED for H not a
+ * multiple of 8 or above 65536, strides not multiples of 8, T or V >= 2^30,
+ * W or Y not 16-byte, ids not 8-byte aligned.
+ */
+lt_status lt_embed_fwd(const int64_t* ids, const lt_half* W, int64_t ldw,
+                       float scale, lt_half* Y, int64_t ldy, int64_t T,
+                       int64_t H, int64_t V, lt_stream stream);
+
+/*
+ * Its gradient: dW[v] = scale * sum over t with ids[t] = v of dY[t], summed in
+ * FP32 in a fixed order (deterministic, no atomics on sums), one rounding.
+ * accumulate = 0 writes all V rows (zeros where no token falls; T may be 0);
+ * accumulate = 1 adds to dW, in FP32 before the rounding, and leaves the rows
+ * without a token as they are.  Padding ids give nothing.  The workspace
+ * (256-byte aligned) needs lt_embed_bwd_workspace_size bytes, 0 for invalid
+ * sizes.  Errors as the forward, and LT_ERR_WORKSPACE.
+ */
+size_t lt_embed_bwd_workspace_size(int64_t T, int64_t H, int64_t V);
+lt_status lt_embed_bwd(const int64_t* ids, const lt_half* dY, int64_t lddy,
+                       float scale, int accumulate, lt_half* dW, int64_t lddw,
+                       void* workspace, size_t ws_bytes, int64_t T, int64_t H,
+                       int64_t V, lt_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,789 @@
+// Attention backward with modified scores, gfx950.
+//
+//   z = cap tanh(scale q.k / cap) - slope |i - j|,  P = exp(z - LSE) on visible pairs
+//   dP = dO V^T,  dZ = P (dP - D),  D_i = rowsum(dO_i * O_i),  dS = dZ (1 - tanh^2)
+//   dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K
+// with dK and dV summed over the query heads of a kv head.  A query that sees no
+// key has dQ = 0, a key that no query sees dK = dV = 0.
+//
+// Kernels, none with an atomic:
+//   1. attn_mod_rows: D_i and the base-2 LSE of every query and head; the
+//      clamped interval of every query and the hull of every 32 queries'
+//      intervals, which the other passes select their blocks by.  HBM-bound.
+//   2. attn_mod_dkdv: key-major.  One workgroup per (batch, kv head, 256-key
+//      tile); each of 8 waves owns 32 keys, with their K fragments and the dK, dV
+//      accumulators in registers.  It lists the 64-query blocks that see some of
+//      its keys, then streams (query head, listed block) pairs HBM -> LDS, double-
+//      buffered.  S = Q K^T and dP = dO V^T put one key in a lane, so that P and
+//      dS feed the dV / dK products from registers.  A wave skips the 32-query
+//      groups that see none of its keys and compares key against interval only
+//      where a group sees them in part.  It stores dS as FP16 blocks of 32 x 32 (the
+//      rounding of any FP16 matrix operand).  Few workgroups: 128-key tiles whose
+//      wave pairs share keys and split the queries, and shares of a tile's pairs
+//      with FP32 partial sums in the workspace, added in order by attn_mod_sum.
+//   3. attn_mod_dq: query-major dQ = scale dS K from the stored blocks.
+// The (batch, kv head) pairs are taken in chunks, 2 and 3 for each, so that the
+// workspace holds one chunk's dS.
+
+#include <type_traits>
+
+#include "attn_mod.hpp"
+
+namespace lt {
+namespace {
+
+// Direct load of 16 bytes per lane into LDS, as lds_dma16_opaque, for data
+// read once (non-temporal).
+__device__ __forceinline__ void lds_dma16_stream(const void* base, uint32_t nrec, void* lds, uint32_t voff) {
+  const uint64_t b = (uint64_t)base;
+  u32x4 r;
+  r[0] = __builtin_amdgcn_readfirstlane((uint32_t)b);
+  r[1] = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32) & 0xffffu);
+  r[2] = __builtin_amdgcn_readfirstlane(nrec);
+  r[3] = 0x00020000u;
+  const uint32_t m0v = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
+               :
+               : "s"(m0v), "v"(voff), "s"(r)
+               : "memory");
+}
+
+constexpr int NWA = 8;         // dK/dV: waves per workgroup
+constexpr int BKV = NWA * 32;  // dK/dV: keys per workgroup (32 per wave)
+constexpr int BQA = 64;        // dK/dV: queries per block (two 32-query halves)
+constexpr int kMaxBlocks = kModMaxS / BQA;
+
+// dS block (query group qg, key group kg) of a head
+__device__ __forceinline__ int64_t ds_block(int qg, int kg, int n32, int causal) {
+  return causal ? (int64_t)qg * (qg + 1) / 2 + kg : (int64_t)qg * n32 + kg;
+}
+
+// ------------------------------------------------------------ 1: row terms, intervals, hulls
+// Workgroups 0 .. n_term - 1: D / 8 lanes per row (one 16-byte chunk each),
+// consecutive queries of one (batch, head); the row's lanes add in a fixed order.
+// The others: 256 queries of one batch row, a lane each.
+template <int D>
+__global__ void __launch_bounds__(256)
+attn_mod_rows_kernel(const lt_half* __restrict__ O, const lt_half* __restrict__ dO, int64_t o_stride,
+                     const float* __restrict__ LSE, float* __restrict__ lse2, float* __restrict__ delta,
+                     const ScoreMod mod, int32_t* __restrict__ rows, QueryHull* __restrict__ hulls,
+                     unsigned n_term, int B, int S, int Hq, int causal) {
+  if (blockIdx.x >= n_term) {
+    const int n_sb = (S + 255) / 256;
+    const int b = (blockIdx.x - n_term) / n_sb;
+    const int q = ((blockIdx.x - n_term) % n_sb) * 256 + threadIdx.x;
+    int lo, hi;
+    row_interval(mod, causal, b, S, q, lo, hi);
+    if (q < S) {
+      rows[(int64_t)b * S + q] = lo;
+      rows[(int64_t)(B + b) * S + q] = hi;
+    }
+    // both halves of the wave are a group of 32
+    const bool some = lo < hi;
+    QueryHull h;
+    h.lo = wave_min32(some ? lo : 0x7fffffff);
+    h.hi = wave_max32(some ? hi : 0);
+    h.all_lo = wave_max32(q >= S ? 0 : some ? lo : 0x7fffffff);
+    h.all_hi = wave_min32(q >= S ? 0x7fffffff : some ? hi : 0);
+    if ((threadIdx.x & 31) == 0 && q < S) hulls[(int64_t)b * ((S + 31) / 32) + q / 32] = h;
+    return;
+  }
+  constexpr int CPR = D / 8;
+  constexpr int RPB = 256 / CPR;                   // rows per workgroup
+  const int n_sb = (S + RPB - 1) / RPB;
+  const int bh = blockIdx.x / n_sb;
+  const int q = (blockIdx.x % n_sb) * RPB + (int)threadIdx.x / CPR;
+  const int c = threadIdx.x % CPR;
+  const int b = bh / Hq;
+  const int h = bh % Hq;
+  float part = 0.f;
+  if (q < S) {
+    const int64_t off = ((int64_t)b * S + q) * o_stride + (int64_t)h * D + c * 8;
+    const half8 x = as_half8(ld16(dO + off));
+    const half8 y = as_half8(ld16(O + off));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part = fmaf((float)x[e], (float)y[e], part);
+  }
+#pragma unroll
+  for (int m = CPR / 2; m >= 1; m >>= 1) part += __shfl_xor(part, m);
+  if (q < S && c == 0) {
+    const int64_t ri = (int64_t)bh * S + q;
+    delta[ri] = part;
+    lse2[ri] = LSE[ri] * kModLog2e;
+  }
+}
+
+// ------------------------------------------------------------ 2: dK/dV
+template <int D>
+struct DkdvSmem {
+  using RT = RowTile<D, NWA>;
+  static constexpr int TQ = BQA * RT::ROWB;             // one Q or dO block
+  // Q and dO buffers first: every fragment read of them is a per-lane
+  // register plus a constant below 64 KiB (the LDS instructions' offset field)
+  static constexpr int Q_OFF = 0;                        // 2 buffers
+  static constexpr int DO_OFF = Q_OFF + 2 * TQ;          // 2 buffers
+  // per buffer five rows of 256 B, a 4-byte direct load of 64 lanes each:
+  // base-2 LSE, D, interval starts and ends, the two hulls
+  static constexpr int NROW = 5;
+  static constexpr int ROW_OFF = DO_OFF + 2 * TQ;
+  static constexpr int V_OFF = ROW_OFF + 2 * NROW * 256; // V tile [BKV][D]
+  static constexpr int BYTES = V_OFF + BKV * RT::ROWB;
+  static_assert(BQA == 64 && DO_OFF + 2 * TQ <= 65536, "one load per row, offsets fit the offset field");
+};
+
+// KSPLIT = 1: 8 key groups of 32 (256 keys), every wave walks both 32-query
+// halves of each block.  KSPLIT = 2: 4 key groups (128 keys); waves w and w + 4
+// own the same keys, take one half each, and their FP32 accumulators are added
+// through LDS at the end.
+template <int D, int KSPLIT, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(NWA * 64, 1)
+attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
+  using SM = DkdvSmem<D>;
+  using RT = RowTile<D, NWA>;
+  constexpr int KK = D / 16;       // MFMA steps over the head dim
+  constexpr int DB = D / 32;       // 32-feature blocks
+  constexpr int NKG = NWA / KSPLIT;                // key groups of 32
+  constexpr int BK = NKG * 32;                     // keys per workgroup
+  static_assert(KSPLIT == 1 || NKG * 2 * DB * 4 * 64 * 16 <= SM::BYTES, "reduction fits in LDS");
+  __shared__ __attribute__((aligned(1024))) char smem[SM::BYTES];
+  __shared__ uint16_t blocks[kMaxBlocks];          // 64-query blocks that see some key of the tile
+  __shared__ int counts[NWA];
+
+  const int B = a.sh.B, S = a.sh.S, Hq = a.sh.Hq, Hkv = a.sh.Hkv, causal = a.sh.causal;
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // uniform: scalar addressing
+  const int lrow = lane & 31;
+  const int g = lane >> 5;
+  const int kg = wave % NKG;                       // key group
+  const int kpart = wave / NKG;                    // query half taken (KSPLIT = 2)
+
+  const int lbkv = blockIdx.x % nb;                // pair within the chunk
+  const int slot = blockIdx.x / nb;
+  const int nsh = a.plan.nsplit;
+  const int jt = slot / nsh;                       // key tile
+  const int sp = slot % nsh;                       // share of its pairs
+  const int b = (bkv0 + lbkv) / Hkv;
+  const int kvh = (bkv0 + lbkv) % Hkv;
+  const int G = Hq / Hkv;
+  const int n32 = (S + 31) / 32;
+  const int kbase = jt * BK;
+  const int kw0 = kbase + kg * 32;                 // this wave's first key
+  const int mykey = kw0 + lrow;                    // key owned by this lane (S, dP columns)
+
+  const lt_half* Kp = a.K + (int64_t)b * S * a.kv_stride + (int64_t)kvh * D;
+  const lt_half* Vp = a.V + (int64_t)b * S * a.kv_stride + (int64_t)kvh * D;
+  const QueryHull* hulls = a.hulls + (int64_t)b * n32;
+
+  // ---- V tile -> LDS (B operand of dP = dO V^T); rows past S read as zero ----
+  RT::template dma<BK>(smem + SM::V_OFF, Vp + (int64_t)kbase * a.kv_stride, a.kv_stride, S - kbase, wave, lane);
+  // ---- K fragments (B operand of S = Q K^T) ----
+  half8 kf[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk)
+    kf[kk] = mykey < S ? as_half8(ld16(Kp + (int64_t)mykey * a.kv_stride + kk * 16 + g * 8))
+                       : as_half8(u32x4{0, 0, 0, 0});
+
+  // ---- list the tile's query blocks, ascending ----
+  const int n_qb = (S + BQA - 1) / BQA;
+  int n_list = 0;
+  for (int i0 = 0; i0 < n_qb; i0 += NWA * 64) {
+    const int i = i0 + tid;
+    bool sees = false;
+    if (i < n_qb) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int qg = 2 * i + u;
+        if (qg < n32) {
+          const QueryHull h = hulls[qg];
+          sees |= h.lo < kbase + BK && h.hi > kbase;
+        }
+      }
+    }
+    const uint64_t bal = __builtin_amdgcn_ballot_w64(sees);
+    if (lane == 0) counts[wave] = __popcll(bal);
+    __syncthreads();
+    int at = n_list;
+#pragma unroll
+    for (int w = 0; w < NWA; ++w) {
+      if (w < wave) at += counts[w];
+      n_list += counts[w];
+    }
+    if (sees) blocks[at + __popcll(bal & ((1ull << lane) - 1))] = (uint16_t)i;
+    __syncthreads();
+  }
+  n_list = __builtin_amdgcn_readfirstlane(n_list);
+
+  // lane part of the row-fragment address of step kk (rows rb + lane % 32,
+  // rb a multiple of 16, so the swizzle depends on the lane only)
+  uint32_t rlane[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) rlane[kk] = (uint32_t)RT::addr(lane & 31, kk * 2 + (lane >> 5));
+  const uint32_t vrow0 = __builtin_amdgcn_readfirstlane(SM::V_OFF + kg * 32 * RT::ROWB);
+
+  f32x16 dkacc[DB], dvacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      dkacc[db][r] = 0.f;
+      dvacc[db][r] = 0.f;
+    }
+
+  const float scale = a.sh.scale;
+  const float c = scale * kModLog2e;
+  const Cap cap(a.mod.cap, scale);
+  // The (query head, listed block) pairs, head-major, in nsh contiguous shares.
+  // Within a head the blocks run last to first: the key tiles of one kv head
+  // (on one XCD by the workgroup order) then move in step under a causal mask,
+  // and share each Q / dO block through that XCD's L2.
+  const int total = G * n_list;
+  const int it0 = (int)((int64_t)sp * total / nsh);
+  const int n_iter = (int)((int64_t)(sp + 1) * total / nsh) - it0;
+  auto pair_of = [&](int i, int& j, int& qbase) {   // j: query head within the group
+    const int it = it0 + i;
+    j = it / n_list;
+    qbase = __builtin_amdgcn_readfirstlane((int)blocks[n_list - 1 - it % n_list]) * BQA;
+  };
+  // Q, dO, LSE, D and the intervals of queries past S read as zero: they see nothing
+  auto stage = [&](int j, int qbase, int buf) {
+    const int h = kvh * G + j;
+    RT::template dma<BQA>(smem + SM::Q_OFF + buf * SM::TQ,
+                          a.Q + ((int64_t)b * S + qbase) * a.q_stride + (int64_t)h * D, a.q_stride, S - qbase,
+                          wave, lane);
+    RT::template dma<BQA>(smem + SM::DO_OFF + buf * SM::TQ,
+                          a.dO + ((int64_t)b * S + qbase) * a.o_stride + (int64_t)h * D, a.o_stride, S - qbase,
+                          wave, lane);
+    if (wave < SM::NROW) {
+      const int nv = S - qbase < BQA ? S - qbase : BQA;
+      const void* src = wave == 0   ? (const void*)(a.lse2 + ((int64_t)b * Hq + h) * S + qbase)
+                        : wave == 1 ? (const void*)(a.delta + ((int64_t)b * Hq + h) * S + qbase)
+                        : wave == 2 ? (const void*)(a.rows + (int64_t)b * S + qbase)
+                        : wave == 3 ? (const void*)(a.rows + (int64_t)(B + b) * S + qbase)
+                                    : (const void*)(hulls + qbase / 32);
+      const int n = wave < 4 ? nv : (nv > 32 ? 2 : 1) * (int)(sizeof(QueryHull) / 4);
+      lds_dma4_opaque(src, (uint32_t)(n * 4), smem + SM::ROW_OFF + (buf * SM::NROW + wave) * 256,
+                      (uint32_t)(lane * 4));
+    }
+  };
+
+  int j = 0, qbase = 0;                            // of the current pair
+  if (n_iter > 0) {
+    pair_of(0, j, qbase);
+    stage(j, qbase, 0);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) loaded_here(kf[kk]);
+
+  // two pairs per trip, so that the buffer index is a constant
+  auto iteration = [&](int it, auto CUR_) {
+    const int cur = CUR_;   // a constant in the unrolled main path
+    int jn = j, qn = qbase;
+    // that buffer was last read before the previous barrier
+    if (it + 1 < n_iter) {
+      pair_of(it + 1, jn, qn);
+      stage(jn, qn, cur ^ 1);
+    }
+    const int h = kvh * G + j;
+    const char* qs = smem + SM::Q_OFF + cur * SM::TQ;
+    const char* dos = smem + SM::DO_OFF + cur * SM::TQ;
+    const char* rowp = smem + SM::ROW_OFF + cur * SM::NROW * 256;
+    const float* lse_s = reinterpret_cast<const float*>(rowp);
+    const float* del_s = reinterpret_cast<const float*>(rowp + 256);
+    const int* lo_s = reinterpret_cast<const int*>(rowp + 512);
+    const int* hi_s = reinterpret_cast<const int*>(rowp + 768);
+    const float slope2 = BIAS ? a.mod.slopes[h] * kModLog2e : 0.f;
+
+    auto half = [&](int ih) {
+      const int hq = KSPLIT > 1 ? kpart : ih;
+      const int qh = qbase + hq * 32;              // 32-query half hq of the block
+      const int4 hv = *reinterpret_cast<const int4*>(rowp + 1024 + hq * 16);
+      const int hlo = __builtin_amdgcn_readfirstlane(hv.x);
+      const int hhi = __builtin_amdgcn_readfirstlane(hv.y);
+      const int all_lo = __builtin_amdgcn_readfirstlane(hv.z);
+      const int all_hi = __builtin_amdgcn_readfirstlane(hv.w);
+      if (qh < S && hlo < kw0 + 32 && hhi > kw0) { // wave-uniform
+        f32x16 sacc, pacc;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sacc[r] = 0.f;
+          pacc[r] = 0.f;
+        }
+        // fragments of step kk+1 are read before the MFMAs of step kk; the Q
+        // and dO reads are a lane register plus a constant, the V read's address
+        // is added right before it (kept there: holding eight V addresses
+        // through the loop does not fit the register budget)
+        auto rdq = [&](int kk) {
+          return as_half8(*reinterpret_cast<const u32x4*>(smem + SM::Q_OFF + cur * SM::TQ + hq * 32 * RT::ROWB +
+                                                          rlane[kk]));
+        };
+        auto rdo = [&](int kk) {
+          return as_half8(*reinterpret_cast<const u32x4*>(smem + SM::DO_OFF + cur * SM::TQ + hq * 32 * RT::ROWB +
+                                                          rlane[kk]));
+        };
+        auto rdv = [&](int kk) {
+          uint32_t ad;
+          asm volatile("v_add_u32 %0, %1, %2" : "=v"(ad) : "v"(rlane[kk]), "s"(vrow0));
+          return as_half8(*reinterpret_cast<const u32x4*>(smem + ad));
+        };
+        half8 fq = rdq(0);
+        half8 fd = rdo(0);
+        half8 fv = rdv(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          half8 nq = fq, nd = fd, nv = fv;
+          if (kk + 1 < KK) {
+            nq = rdq(kk + 1);
+            nd = rdo(kk + 1);
+            nv = rdv(kk + 1);
+          }
+          sacc = mfma32(fq, kf[kk], sacc);
+          pacc = mfma32(fd, fv, pacc);
+          if (kk + 1 < KK) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);   // the three reads
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);   // then the two MFMAs
+          }
+          fq = nq;
+          fd = nd;
+          fv = nv;
+        }
+        __builtin_amdgcn_s_setprio(0);
+        // P = exp2(z - LSE2), dS = P (dP - D) (1 - tanh^2)
+        float p[16], ds[16];
+        const float d0 = (float)(qh + 4 * g - mykey);
+#pragma unroll
+        for (int rq = 0; rq < 4; ++rq) {
+          const int ql0 = hq * 32 + 8 * rq + 4 * g;
+          const float4 l4 = *reinterpret_cast<const float4*>(lse_s + ql0);
+          const float4 d4 = *reinterpret_cast<const float4*>(del_s + ql0);
+          const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
+          const float dv[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * rq + e;
+            float z, w = 1.f;
+            if constexpr (CAP) {
+              const float u = cap.u(sacc[r]);
+              const float u4 = 4.f * u;
+              w = fmaf(-u4, u, u4);
+              z = cap.z(u) - lv[e];
+            } else {
+              z = fmaf(sacc[r], c, -lv[e]);
+            }
+            if constexpr (BIAS) z = fmaf(-slope2, fabsf(d0 + (float)(8 * rq + e)), z);
+            p[r] = fast_exp2(z);
+            ds[r] = CAP ? (pacc[r] - dv[e]) * w : pacc[r] - dv[e];
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ds[r] *= p[r];
+        if (kw0 < all_lo || kw0 + 32 > all_hi) {   // wave-uniform: some query sees them in part
+#pragma unroll
+          for (int rq = 0; rq < 4; ++rq) {
+            const int ql0 = hq * 32 + 8 * rq + 4 * g;
+            const int4 l4 = *reinterpret_cast<const int4*>(lo_s + ql0);
+            const int4 h4 = *reinterpret_cast<const int4*>(hi_s + ql0);
+            const int lv[4] = {l4.x, l4.y, l4.z, l4.w};
+            const int hw[4] = {h4.x, h4.y, h4.z, h4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool see = (mykey >= lv[e]) & (mykey < hw[e]);
+              p[4 * rq + e] = see ? p[4 * rq + e] : 0.f;
+              ds[4 * rq + e] = see ? ds[4 * rq + e] : 0.f;
+            }
+          }
+        }
+        half8 pp[2], pds[2];
+#pragma unroll
+        for (int kc = 0; kc < 2; ++kc) {
+          pp[kc] = pack8(p[8 * kc], p[8 * kc + 1], p[8 * kc + 2], p[8 * kc + 3], p[8 * kc + 4],
+                         p[8 * kc + 5], p[8 * kc + 6], p[8 * kc + 7]);
+          pds[kc] = pack8(ds[8 * kc], ds[8 * kc + 1], ds[8 * kc + 2], ds[8 * kc + 3],
+                          ds[8 * kc + 4], ds[8 * kc + 5], ds[8 * kc + 6], ds[8 * kc + 7]);
+        }
+        // dS block for the dQ pass, as held here (lane-major, 32 bytes per
+        // lane); written once, read once: non-temporal
+        {
+          const int64_t nblk = causal ? (int64_t)n32 * (n32 + 1) / 2 : (int64_t)n32 * n32;
+          char* dst = reinterpret_cast<char*>(a.ds) +
+                      (((int64_t)lbkv * G + j) * nblk + ds_block(qh >> 5, kw0 >> 5, n32, causal)) * kDsBlockBytes +
+                      lane * 32;
+          __builtin_nontemporal_store(as_u32x4(pds[0]), reinterpret_cast<u32x4*>(dst));
+          __builtin_nontemporal_store(as_u32x4(pds[1]), reinterpret_cast<u32x4*>(dst + 16));
+        }
+        __builtin_amdgcn_s_setprio(1);
+        //   dV^T += dO^T P,  dK^T += Q^T dS
+        // steps (kc, db): the transposed dO and Q fragments of step s + 1 are
+        // read before step s's two MFMAs, into the other of two register sets
+        constexpr int NST = 2 * DB;
+        half8 tdo[2], tq[2];
+        auto rd_tr = [&](int st_, half8& x, half8& y) {
+          const int kc = st_ / DB, db = st_ % DB;
+          x = RT::template tr_frag<true>(dos, hq * 32 + kc * 16, db * 32, lane);
+          y = RT::template tr_frag<true>(qs, hq * 32 + kc * 16, db * 32, lane);
+        };
+        rd_tr(0, tdo[0], tq[0]);
+#pragma unroll
+        for (int st_ = 0; st_ < NST; ++st_) {
+          const int kc = st_ / DB, db = st_ % DB;
+          if (st_ + 1 < NST) rd_tr(st_ + 1, tdo[(st_ + 1) & 1], tq[(st_ + 1) & 1]);
+          dvacc[db] = mfma32(tdo[st_ & 1], pp[kc], dvacc[db]);
+          dkacc[db] = mfma32(tq[st_ & 1], pds[kc], dkacc[db]);
+          // the groups count from the top of the block: the first read group
+          // holds steps 0 and 1 (two transposed reads per fragment)
+          if (st_ + 1 < NST) {
+            if (st_ == 0)
+              __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+            else
+              __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+          }
+        }
+        __builtin_amdgcn_s_setprio(0);
+      }
+    };
+    if constexpr (KSPLIT == 1) {
+#pragma unroll
+      for (int ih = 0; ih < BQA / 32; ++ih) half(ih);
+    } else {
+      half(0);
+    }
+    j = jn;
+    qbase = qn;
+    // next block resident for every wave; nobody reads this buffer any more
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  if constexpr (KSPLIT == 1) {
+    for (int it = 0; it < n_iter; it += 2) {
+      iteration(it, std::integral_constant<int, 0>{});
+      if (it + 1 < n_iter) iteration(it + 1, std::integral_constant<int, 1>{});
+    }
+  } else {
+    for (int it = 0; it < n_iter; ++it) iteration(it, it & 1);
+  }
+
+  if constexpr (KSPLIT > 1) {
+    // all of LDS is free after the loop's last barrier: the second wave of
+    // each pair passes its dK, dV accumulators through it (lane-major float4,
+    // conflict-free) to the first, which adds them
+    float4* red = reinterpret_cast<float4*>(smem);
+    auto at = [&](int which, int db, int rq) { return (((kg * 2 + which) * DB + db) * 4 + rq) * 64 + lane; };
+    if (kpart == 1) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int rq = 0; rq < 4; ++rq) {
+          red[at(0, db, rq)] = make_float4(dkacc[db][4 * rq], dkacc[db][4 * rq + 1], dkacc[db][4 * rq + 2],
+                                           dkacc[db][4 * rq + 3]);
+          red[at(1, db, rq)] = make_float4(dvacc[db][4 * rq], dvacc[db][4 * rq + 1], dvacc[db][4 * rq + 2],
+                                           dvacc[db][4 * rq + 3]);
+        }
+    }
+    __syncthreads();
+    if (kpart != 0) return;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq) {
+        const float4 k = red[at(0, db, rq)];
+        const float4 v = red[at(1, db, rq)];
+        const float kv[4] = {k.x, k.y, k.z, k.w}, vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          dkacc[db][4 * rq + e] += kv[e];
+          dvacc[db][4 * rq + e] += vv[e];
+        }
+      }
+  }
+
+  // ---- write dK = scale * acc, dV (or this share's FP32 partial sums) ----
+  if (mykey >= S) return;
+  if (nsh > 1) {
+    float* pk = a.part + (((int64_t)lbkv * nsh + sp) * S + mykey) * D;
+    float* pv = pk + (int64_t)nb * nsh * S * D;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq) {
+        const int d = db * 32 + 8 * rq + 4 * g;
+        *reinterpret_cast<float4*>(pk + d) = make_float4(dkacc[db][4 * rq], dkacc[db][4 * rq + 1],
+                                                         dkacc[db][4 * rq + 2], dkacc[db][4 * rq + 3]);
+        *reinterpret_cast<float4*>(pv + d) = make_float4(dvacc[db][4 * rq], dvacc[db][4 * rq + 1],
+                                                         dvacc[db][4 * rq + 2], dvacc[db][4 * rq + 3]);
+      }
+  } else {
+    lt_half* dkp = a.dK + ((int64_t)b * S + mykey) * a.dkv_stride + (int64_t)kvh * D;
+    lt_half* dvp = a.dV + ((int64_t)b * S + mykey) * a.dkv_stride + (int64_t)kvh * D;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq) {
+        half4 k4, v4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          k4[e] = (_Float16)(dkacc[db][4 * rq + e] * scale);
+          v4[e] = (_Float16)dvacc[db][4 * rq + e];
+        }
+        *reinterpret_cast<half4*>(dkp + db * 32 + 8 * rq + 4 * g) = k4;
+        *reinterpret_cast<half4*>(dvp + db * 32 + 8 * rq + 4 * g) = v4;
+      }
+  }
+}
+
+// dK = scale * sum of the shares' partials, dV = sum, in share order.  HBM-bound.
+template <int D>
+__global__ void __launch_bounds__(256)
+attn_mod_sum_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
+  constexpr int CPR = D / 8;                       // 8-element chunks per row
+  const int S = a.sh.S, Hkv = a.sh.Hkv, nsh = a.plan.nsplit;
+  const int64_t gid = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (gid >= (int64_t)nb * S * CPR) return;
+  const int d0 = (int)(gid % CPR) * 8;
+  const int key = (int)((gid / CPR) % S);
+  const int lbkv = (int)(gid / ((int64_t)CPR * S));
+  const int b = (bkv0 + lbkv) / Hkv, kvh = (bkv0 + lbkv) % Hkv;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const float* src = a.part + (((int64_t)(which * nb + lbkv) * nsh) * S + key) * D + d0;
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < nsh; ++t) {
+      const float4 x = *reinterpret_cast<const float4*>(src + (int64_t)t * S * D);
+      const float4 y = *reinterpret_cast<const float4*>(src + (int64_t)t * S * D + 4);
+      acc[0] += x.x; acc[1] += x.y; acc[2] += x.z; acc[3] += x.w;
+      acc[4] += y.x; acc[5] += y.y; acc[6] += y.z; acc[7] += y.w;
+    }
+    const float f = which == 0 ? a.sh.scale : 1.f;
+    const half8 o = pack8(acc[0] * f, acc[1] * f, acc[2] * f, acc[3] * f, acc[4] * f, acc[5] * f, acc[6] * f,
+                          acc[7] * f);
+    st16((which == 0 ? a.dK : a.dV) + ((int64_t)b * S + key) * a.dkv_stride + (int64_t)kvh * D + d0, as_u32x4(o));
+  }
+}
+
+// ------------------------------------------------------------ 3: dQ from dS
+constexpr int BKQ = 64;         // keys per slice (two 32-key groups)
+
+// NWQ waves per workgroup, one 32-query group each; two slices in flight while
+// one is used (three for the smaller workgroups).
+template <int D, int NWQ>
+struct DqSmem {
+  using RT = RowTile<D, NWQ>;
+  static constexpr int NS = NWQ == 8 ? 3 : 4;
+  static constexpr int KT = BKQ * RT::ROWB;          // K slice [64][D]
+  static constexpr int DSW = 2 * kDsBlockBytes;      // one wave's two dS blocks of a slice
+  static constexpr int STAGE = KT + NWQ * DSW;
+  static constexpr int BYTES = NS * STAGE;
+  // direct loads per wave and stage: K rows, then always four 1 KiB dS loads
+  // (of blocks that the mask drops a zero-length buffer), so that the count
+  // behind each vmcnt wait is fixed
+  static constexpr int LOADS = KT / 1024 / NWQ + 4;
+};
+
+// B operand dS^T of dQ^T = K^T dS^T from one dS block in LDS (lane-major,
+// 32 bytes per lane of the dK/dV pass): lane L gets stored query position
+// L % 32 at keys kb + 8 (j / 4) + 4 (L / 32) + j % 4, j = 0..7 (the key order of
+// RowTile::tr_frag<true>).
+__device__ __forceinline__ half8 ds_tr_frag(const char* blk, int kb, int lane) {
+  v4s part[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int k = kb + 8 * h + 4 * (lane >> 5) + ((lane & 15) >> 2);
+    part[h] = lds_read_tr16(blk + (k + 32 * ((lane >> 4) & 1)) * 32 + 8 * (lane & 3));
+  }
+  return as_half8(pack_v4s_pair(part[0], part[1]));
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt field");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+template <int D, int NWQ>
+__global__ void __launch_bounds__(NWQ * 64, 1)
+attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
+  using SM = DqSmem<D, NWQ>;
+  using RT = RowTile<D, NWQ>;
+  constexpr int BQQ = NWQ * 32;                    // queries per workgroup
+  constexpr int NSQ = SM::NS;
+  constexpr int DB = D / 32;
+  static_assert(SM::BYTES <= 160 * 1024, "stages fit in LDS");
+  __shared__ __attribute__((aligned(1024))) char smem[SM::BYTES];
+
+  const int S = a.sh.S, Hq = a.sh.Hq, Hkv = a.sh.Hkv, causal = a.sh.causal;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n32 = (S + 31) / 32;
+  const int n_qt = (S + BQQ - 1) / BQQ;
+  const int G = Hq / Hkv;
+  const int slot = blockIdx.x / (nb * G);
+  const int qt = causal ? n_qt - 1 - slot : slot;
+  // the query heads of one kv head on one XCD where the chunk is a multiple of 8
+  const int lbkv = (blockIdx.x % (nb * G)) % nb;
+  const int j = (blockIdx.x % (nb * G)) / nb;
+  const int b = (bkv0 + lbkv) / Hkv;
+  const int kvh = (bkv0 + lbkv) % Hkv;
+  const int h = kvh * G + j;
+  const int qg = qt * NWQ + wave;                  // this wave's 32-query group
+  const QueryHull* hulls = a.hulls + (int64_t)b * n32;
+  // key groups that some query of the group, of the workgroup, sees
+  int kg0 = 0, kg_end = 0, wg_lo = 0x7fffffff, wg_hi = 0;
+#pragma unroll
+  for (int w = 0; w < NWQ; ++w) {
+    const int q = qt * NWQ + w;
+    if (q < n32) {
+      const int lo = hulls[q].lo, hi = hulls[q].hi;
+      wg_lo = min(wg_lo, lo);
+      wg_hi = max(wg_hi, hi);
+      if (w == wave && lo < hi) {
+        kg0 = lo >> 5;
+        kg_end = (hi + 31) >> 5;
+      }
+    }
+  }
+  kg0 = __builtin_amdgcn_readfirstlane(kg0);
+  kg_end = __builtin_amdgcn_readfirstlane(kg_end);
+  const int ks0 = __builtin_amdgcn_readfirstlane(wg_lo < wg_hi ? wg_lo / BKQ : 0);
+  const int n_ks = __builtin_amdgcn_readfirstlane(wg_lo < wg_hi ? (wg_hi + BKQ - 1) / BKQ - ks0 : 0);
+
+  const lt_half* Kp = a.K + (int64_t)b * S * a.kv_stride + (int64_t)kvh * D;
+  const int64_t nblk = causal ? (int64_t)n32 * (n32 + 1) / 2 : (int64_t)n32 * n32;
+  // block (qg, 0); block (qg, kg) follows at kg * 2 KiB
+  const char* dsq = reinterpret_cast<const char*>(a.ds) +
+                    (((int64_t)lbkv * G + j) * nblk + ds_block(qg < n32 ? qg : 0, 0, n32, causal)) * kDsBlockBytes;
+
+  f32x16 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
+
+  // slice i (keys from (ks0 + i) * 64) -> stage i % NSQ; K rows past S read as zero
+  auto stage = [&](int i) {
+    char* st = smem + (i % NSQ) * SM::STAGE;
+    const int ks = ks0 + i;
+    RT::template dma<BKQ>(st, Kp + (int64_t)ks * BKQ * a.kv_stride, a.kv_stride, S - ks * BKQ, wave, lane);
+    char* mine = st + SM::KT + wave * SM::DSW;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int kg = 2 * ks + c;
+      const bool in = kg >= kg0 && kg < kg_end;
+      const char* src = dsq + (int64_t)(in ? kg : 0) * kDsBlockBytes;
+      const uint32_t nrec = in ? kDsBlockBytes : 0u;
+      lds_dma16_stream(src, nrec, mine + c * kDsBlockBytes, (uint32_t)(lane * 16));
+      lds_dma16_stream(src, nrec, mine + c * kDsBlockBytes + 1024, (uint32_t)(1024 + lane * 16));
+    }
+  };
+
+  // slices after the next one may stay in flight, up to NSQ - 2 of them
+  auto wait_next = [&](int behind) {
+    if (behind >= NSQ - 2) wait_vmcnt<(NSQ - 2) * SM::LOADS>();
+    else if (NSQ > 3 && behind == 1) wait_vmcnt<SM::LOADS>();
+    else wait_vmcnt<0>();
+  };
+  for (int i = 0; i < NSQ - 1 && i < n_ks; ++i) stage(i);
+  wait_next(min(NSQ - 1, n_ks) - 1);               // slice 0 resident
+  __syncthreads();
+  for (int i = 0; i < n_ks; ++i) {
+    // the stage of slice i + NSQ - 1 was last read before the previous barrier
+    if (i + NSQ - 1 < n_ks) stage(i + NSQ - 1);
+    const char* st = smem + (i % NSQ) * SM::STAGE;
+    const char* mine = st + SM::KT + wave * SM::DSW;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int kg = 2 * (ks0 + i) + c;
+      if (kg >= kg0 && kg < kg_end) {
+#pragma unroll
+        for (int kc = 0; kc < 2; ++kc) {
+          //   dQ^T += K^T dS^T  (K^T read transposed, keys in accumulator order)
+          const half8 bds = ds_tr_frag(mine + c * kDsBlockBytes, kc * 16, lane);
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+            acc[db] = mfma32(RT::template tr_frag<true>(st, c * 32 + kc * 16, db * 32, lane), bds, acc[db]);
+        }
+      }
+    }
+    // the next slice resident for every wave (later slices' loads may still be
+    // in flight); nobody reads this stage any more
+    wait_next(min(i + NSQ - 1, n_ks - 1) - (i + 1));
+    __syncthreads();
+  }
+
+  // ---- dQ = scale * acc -> FP16; lane L holds stored query position L % 32 ----
+  if (qg < n32) {
+    const int pos = lane & 31;
+    const int q = qg * 32 + 8 * ((pos & 15) >> 2) + 4 * (pos >> 4) + (pos & 3);
+    const int g = lane >> 5;
+    if (q < S) {
+      lt_half* qp = a.dQ + ((int64_t)b * S + q) * a.dq_stride + (int64_t)h * D;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int rq = 0; rq < 4; ++rq) {
+          half4 o;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = (_Float16)(acc[db][4 * rq + e] * a.sh.scale);
+          *reinterpret_cast<half4*>(qp + db * 32 + 8 * rq + 4 * g) = o;
+        }
+    }
+  }
+}
+
+constexpr int64_t kDqHalfWgs = 128;   // 256-query workgroups up to which they hold 128
+
+template <int D, bool CAP, bool BIAS>
+hipError_t launch_bwd(const AttnModBwdArgs& a, hipStream_t s) {
+  const AttnShape& sh = a.sh;
+  constexpr int rpb = 256 / (D / 8);
+  const unsigned n_term = (unsigned)((int64_t)sh.B * sh.Hq * ((sh.S + rpb - 1) / rpb));
+  const unsigned n_rows = (unsigned)((int64_t)sh.B * ((sh.S + 255) / 256));
+  hipLaunchKernelGGL((attn_mod_rows_kernel<D>), dim3(n_term + n_rows), dim3(256), 0, s, a.O, a.dO, a.o_stride, a.LSE,
+                     a.lse2, a.delta, a.mod, a.rows, a.hulls, n_term, sh.B, sh.S, sh.Hq, sh.causal);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int pairs = sh.B * sh.Hkv, grp = sh.Hq / sh.Hkv;
+  const int n_kt = (sh.S + a.plan.ktile - 1) / a.plan.ktile;
+  for (int bkv0 = 0; bkv0 < pairs; bkv0 += a.plan.chunk) {
+    const int nb = pairs - bkv0 < a.plan.chunk ? pairs - bkv0 : a.plan.chunk;
+    const dim3 kgrid((unsigned)((int64_t)n_kt * a.plan.nsplit * nb));
+    if (a.plan.ktile == BKV)
+      hipLaunchKernelGGL((attn_mod_dkdv_kernel<D, 1, CAP, BIAS>), kgrid, dim3(NWA * 64), 0, s, a, bkv0, nb);
+    else
+      hipLaunchKernelGGL((attn_mod_dkdv_kernel<D, 2, CAP, BIAS>), kgrid, dim3(NWA * 64), 0, s, a, bkv0, nb);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (a.plan.nsplit > 1) {
+      const int64_t chunks = (int64_t)nb * sh.S * (D / 8);
+      hipLaunchKernelGGL((attn_mod_sum_kernel<D>), dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, a, bkv0,
+                         nb);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    // longest query tiles first under a causal mask
+    auto launch_dq = [&](auto W_) {
+      constexpr int NWQ = decltype(W_)::value;
+      const int n_qt = (sh.S + NWQ * 32 - 1) / (NWQ * 32);
+      hipLaunchKernelGGL((attn_mod_dq_kernel<D, NWQ>), dim3((unsigned)((int64_t)n_qt * nb * grp)), dim3(NWQ * 64), 0,
+                         s, a, bkv0, nb);
+    };
+    if ((int64_t)((sh.S + 255) / 256) * nb * grp > kDqHalfWgs) launch_dq(std::integral_constant<int, 8>{});
+    else launch_dq(std::integral_constant<int, 4>{});
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  return e;
+}
+
+template <int D>
+hipError_t launch_bwd_d(const AttnModBwdArgs& a, hipStream_t s) {
+  if (a.mod.cap > 0.f) return a.mod.slopes ? launch_bwd<D, true, true>(a, s) : launch_bwd<D, true, false>(a, s);
+  return a.mod.slopes ? launch_bwd<D, false, true>(a, s) : launch_bwd<D, false, false>(a, s);
+}
+
+}  // namespace
+
+hipError_t attn_mod_bwd_launch(const AttnModBwdArgs& a, hipStream_t s) {
+  return a.sh.D == 128 ? launch_bwd_d<128>(a, s) : launch_bwd_d<64>(a, s);
+}
+
+}  // namespace lt

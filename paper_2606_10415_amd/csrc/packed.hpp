@@ -1,0 +1,150 @@
+// Internal launcher interface of the packed-sequence operators (attention with
+// modified scores, QK norm with rotation, embedding): packed_api.cpp checks
+// the arguments, then calls these.
+#pragma once
+
+#include "kernels.hpp"
+
+namespace lt {
+
+// ---------------------------------------------------------------- attention with modified scores
+// Which scores there are and what becomes of them.  Query i of batch row b
+// sees the keys lo <= j < hi (row_interval in attn_mod.hpp).
+struct ScoreMod {
+  const int32_t* lo;      // [B, S] first visible key, or null: 0
+  const int32_t* hi;      // [B, S] end of the visible keys, or null: S
+  const float* slopes;    // [Hq] distance bias, or null: none
+  float cap;              // tanh cap, 0: none
+};
+
+struct AttnModFwdArgs {
+  AttnShape sh;
+  ScoreMod mod;
+  const lt_half* Q;
+  const lt_half* K;
+  const lt_half* V;
+  int64_t q_stride, kv_stride;
+  lt_half* O;
+  int64_t o_stride;
+  float* LSE;
+};
+
+// The hull of a group of 32 queries: some query of the group sees keys
+// lo .. hi - 1 (none: lo >= hi), every query of it sees keys all_lo .. all_hi - 1.
+struct QueryHull {
+  int lo, hi, all_lo, all_hi;
+};
+
+// How the backward is launched.  The (batch, kv head) pairs are taken `chunk`
+// at a time, each chunk's dK/dV pass followed by its dQ pass, so that the dS
+// blocks in the workspace are one chunk's: a chunk is as large as keeps them
+// within kModDsBudget, but has at least the workgroups to fill the CUs twice.
+// ktile and nsplit as in DkdvPlan, for one chunk; the shares of a key tile are
+// equal parts of its (query head, visible 64-query block) pairs.
+constexpr int64_t kModDsBudget = (int64_t)4 << 30;
+constexpr int kModMaxS = 1 << 19;         // the dK/dV pass lists a tile's 64-query blocks in LDS
+struct AttnModPlan {
+  int chunk, ktile, nsplit;
+};
+inline AttnModPlan attn_mod_plan(int B, int S, int Hq, int Hkv, int causal) {
+  const int64_t pairs = (int64_t)B * Hkv, grp = Hq / Hkv;
+  const int64_t per_pair = grp * attn_bwd_ds_blocks(S, causal) * kDsBlockBytes;
+  const int64_t n_kt = ((int64_t)S + 255) / 256;
+  int64_t fill = 512 / (n_kt * grp);
+  int64_t fit = kModDsBudget / per_pair;
+  int64_t c = fit > fill ? fit : fill;
+  c = c < 1 ? 1 : c > pairs ? pairs : c;
+  const int64_t chunks = (pairs + c - 1) / c;
+  c = (pairs + chunks - 1) / chunks;
+  const DkdvPlan p = attn_bwd_dkdv_plan(1, S, (int)(c * grp), (int)c);
+  return {(int)c, p.ktile, p.nsplit};
+}
+// Workspace parts of the backward, in order, each 256-byte aligned: D and the
+// base-2 LSE [B, Hq, S] FP32, the rows' intervals [2][B, S] and the hulls
+// [B][ceil(S / 32)], one chunk's dS blocks, one chunk's partial dK and dV.
+struct AttnModWs {
+  size_t lse2, rows, hulls, ds, part, total;
+};
+inline AttnModWs attn_mod_ws(int B, int S, int Hq, int Hkv, int D, int causal) {
+  const AttnModPlan p = attn_mod_plan(B, S, Hq, Hkv, causal);
+  const size_t n32 = ((size_t)S + 31) / 32;
+  AttnModWs w;
+  w.lse2 = align256((size_t)B * Hq * S * sizeof(float));
+  w.rows = 2 * w.lse2;
+  w.hulls = w.rows + align256((size_t)2 * B * S * sizeof(int32_t));
+  w.ds = w.hulls + align256((size_t)B * n32 * sizeof(QueryHull));
+  w.part = w.ds + align256((size_t)p.chunk * (Hq / Hkv) * (size_t)attn_bwd_ds_blocks(S, causal) * kDsBlockBytes);
+  w.total = w.part + (p.nsplit > 1 ? align256((size_t)2 * p.chunk * p.nsplit * S * D * sizeof(float)) : 0);
+  return w;
+}
+
+struct AttnModBwdArgs {
+  AttnShape sh;
+  ScoreMod mod;
+  const lt_half* Q;
+  const lt_half* K;
+  const lt_half* V;
+  int64_t q_stride, kv_stride;
+  const lt_half* O;
+  const lt_half* dO;
+  int64_t o_stride;
+  const float* LSE;
+  lt_half* dQ;
+  lt_half* dK;
+  lt_half* dV;
+  int64_t dq_stride, dkv_stride;
+  AttnModPlan plan;
+  float* delta;           // workspace, see AttnModWs
+  float* lse2;
+  int32_t* rows;
+  QueryHull* hulls;
+  lt_half* ds;
+  float* part;
+};
+
+hipError_t attn_mod_fwd_launch(const AttnModFwdArgs& a, hipStream_t s);
+hipError_t attn_mod_bwd_launch(const AttnModBwdArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- QK norm with rotation
+struct QkNormArgs {
+  const lt_half* X;       // [T, >= (Hq + Hkv) D] heads before the norm
+  int64_t ldx;
+  const lt_half* Wq;      // [D] norm weights
+  const lt_half* Wk;
+  const float* CS;        // [P][D / 2] (cos, sin)
+  int P;
+  const int32_t* POS;     // [T] or null: t % S
+  int64_t T;
+  int S, Hq, Hkv, D;
+};
+// dW partial sums: one FP32 row of 2 D per workgroup
+constexpr int kQkNormWaves = 4;
+inline int qknorm_bwd_blocks(int64_t T) {
+  const int64_t b = T / kQkNormWaves + (T % kQkNormWaves != 0);
+  return (int)(b < 1024 ? (b < 1 ? 1 : b) : 1024);
+}
+inline size_t qknorm_bwd_ws_bytes(int64_t T, int D) {
+  return align256((size_t)qknorm_bwd_blocks(T) * 2 * D * sizeof(float));
+}
+hipError_t qknorm_fwd_launch(const QkNormArgs& a, lt_half* Y, int64_t ldy, float* RSTD, float eps, hipStream_t s);
+hipError_t qknorm_bwd_launch(const QkNormArgs& a, const lt_half* dY, int64_t lddy, const float* RSTD, lt_half* dX,
+                             int64_t lddx, lt_half* dWq, lt_half* dWk, float* part, hipStream_t s);
+
+// ---------------------------------------------------------------- embedding
+struct EmbedBwdArgs {
+  const int64_t* ids;
+  const lt_half* dY;
+  int64_t lddy;
+  float scale;
+  int accumulate;
+  lt_half* dW;
+  int64_t lddw;
+  int64_t T, H, V;
+  char* ws;
+};
+inline size_t embed_bwd_ws_bytes(int64_t, int64_t, int64_t) { return 256; }
+hipError_t embed_fwd_launch(const int64_t* ids, const lt_half* W, int64_t ldw, float scale, lt_half* Y, int64_t ldy,
+                            int64_t T, int64_t H, int64_t V, hipStream_t s);
+hipError_t embed_bwd_launch(const EmbedBwdArgs& a, hipStream_t s);
+
+}  // namespace lt

@@ -128,6 +128,28 @@ _lib.lt_rope_table.restype = _int
 _lib.lt_rope_table.argtypes = [_vp, _int, _int, ctypes.c_double, _vp]
 _lib.lt_rope_f16.restype = _int
 _lib.lt_rope_f16.argtypes = [_vp, _i64, _int, _int, _int, _int, _vp, _int, _vp]
+_lib.lt_attn_mod_fwd.restype = _int
+_lib.lt_attn_mod_fwd.argtypes = [_vp, _vp, _vp, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _f32, _int, _int,
+                                 _int, _int, _int, _f32, _int, _vp]
+_lib.lt_attn_mod_bwd_workspace_size.restype = _sz
+_lib.lt_attn_mod_bwd_workspace_size.argtypes = [_int, _int, _int, _int, _int, _int]
+_lib.lt_attn_mod_bwd.restype = _int
+_lib.lt_attn_mod_bwd.argtypes = [_vp, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _f32, _vp, _vp,
+                                 _vp, _i64, _i64, _vp, _sz, _int, _int, _int, _int, _int, _f32, _int, _vp]
+_lib.lt_qknorm_rope_fwd.restype = _int
+_lib.lt_qknorm_rope_fwd.argtypes = [_vp, _i64, _vp, _vp, _vp, _int, _vp, _vp, _i64, _vp, _int, _int, _int, _int,
+                                    _int, _f32, _vp]
+_lib.lt_qknorm_rope_bwd_workspace_size.restype = _sz
+_lib.lt_qknorm_rope_bwd_workspace_size.argtypes = [_int, _int, _int, _int, _int]
+_lib.lt_qknorm_rope_bwd.restype = _int
+_lib.lt_qknorm_rope_bwd.argtypes = [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _int, _vp, _vp, _i64, _vp, _vp, _vp,
+                                    _sz, _int, _int, _int, _int, _int, _vp]
+_lib.lt_embed_fwd.restype = _int
+_lib.lt_embed_fwd.argtypes = [_vp, _vp, _i64, _f32, _vp, _i64, _i64, _i64, _i64, _vp]
+_lib.lt_embed_bwd_workspace_size.restype = _sz
+_lib.lt_embed_bwd_workspace_size.argtypes = [_i64, _i64, _i64]
+_lib.lt_embed_bwd.restype = _int
+_lib.lt_embed_bwd.argtypes = [_vp, _vp, _i64, _f32, _int, _vp, _i64, _vp, _sz, _i64, _i64, _i64, _vp]
 
 
 def status_string(status):
@@ -317,6 +339,70 @@ def lt_rope_table(CS, S, D, base, stream=None):
 def lt_rope_f16(X, row_stride, B, S, heads, D, CS, inverse, stream=None):
     _check(_lib.lt_rope_f16(_ptr(X), int(row_stride), int(B), int(S), int(heads), int(D), _ptr(CS),
                             int(inverse), _stream(stream)), "lt_rope_f16")
+
+
+def _typed(x, dtype, name):
+    """_ptr of an array that is not FP16: a tensor must have the type the library reads."""
+    if x is not None and not isinstance(x, int) and str(x.dtype) != dtype:
+        raise TypeError(f"{name} must be a {dtype} tensor, got {x.dtype}")
+    return _ptr(x)
+
+
+def lt_attn_mod_fwd(Q, K, V, q_row_stride, kv_row_stride, O, o_row_stride, LSE, LO, HI, slopes, cap, B, S, Hq, Hkv,
+                    D, scale, causal, stream=None):
+    _check(_lib.lt_attn_mod_fwd(_ptr(Q), _ptr(K), _ptr(V), int(q_row_stride), int(kv_row_stride), _ptr(O),
+                                int(o_row_stride), _ptr(LSE), _typed(LO, "torch.int32", "LO"),
+                                _typed(HI, "torch.int32", "HI"), _typed(slopes, "torch.float32", "slopes"),
+                                float(cap), int(B), int(S), int(Hq), int(Hkv), int(D), float(scale), int(causal),
+                                _stream(stream)), "lt_attn_mod_fwd")
+
+
+def lt_attn_mod_bwd_workspace_size(B, S, Hq, Hkv, D, causal):
+    return int(_lib.lt_attn_mod_bwd_workspace_size(int(B), int(S), int(Hq), int(Hkv), int(D), int(causal)))
+
+
+def lt_attn_mod_bwd(Q, K, V, q_row_stride, kv_row_stride, O, dO, o_row_stride, LSE, LO, HI, slopes, cap, dQ, dK, dV,
+                    dq_row_stride, dkv_row_stride, workspace, ws_bytes, B, S, Hq, Hkv, D, scale, causal,
+                    stream=None):
+    _check(_lib.lt_attn_mod_bwd(_ptr(Q), _ptr(K), _ptr(V), int(q_row_stride), int(kv_row_stride), _ptr(O), _ptr(dO),
+                                int(o_row_stride), _ptr(LSE), _typed(LO, "torch.int32", "LO"),
+                                _typed(HI, "torch.int32", "HI"), _typed(slopes, "torch.float32", "slopes"),
+                                float(cap), _ptr(dQ), _ptr(dK), _ptr(dV), int(dq_row_stride), int(dkv_row_stride),
+                                _ptr(workspace), int(ws_bytes), int(B), int(S), int(Hq), int(Hkv), int(D),
+                                float(scale), int(causal), _stream(stream)), "lt_attn_mod_bwd")
+
+
+def lt_qknorm_rope_fwd(X, ldx, Wq, Wk, CS, P, POS, Y, ldy, RSTD, B, S, Hq, Hkv, D, eps, stream=None):
+    _check(_lib.lt_qknorm_rope_fwd(_ptr(X), int(ldx), _ptr(Wq), _ptr(Wk), _ptr(CS), int(P),
+                                   _typed(POS, "torch.int32", "POS"), _ptr(Y), int(ldy), _ptr(RSTD), int(B), int(S),
+                                   int(Hq), int(Hkv), int(D), float(eps), _stream(stream)), "lt_qknorm_rope_fwd")
+
+
+def lt_qknorm_rope_bwd_workspace_size(B, S, Hq, Hkv, D):
+    return int(_lib.lt_qknorm_rope_bwd_workspace_size(int(B), int(S), int(Hq), int(Hkv), int(D)))
+
+
+def lt_qknorm_rope_bwd(dY, lddy, X, ldx, Wq, Wk, RSTD, CS, P, POS, dX, lddx, dWq, dWk, workspace, ws_bytes, B, S, Hq,
+                       Hkv, D, stream=None):
+    _check(_lib.lt_qknorm_rope_bwd(_ptr(dY), int(lddy), _ptr(X), int(ldx), _ptr(Wq), _ptr(Wk), _ptr(RSTD), _ptr(CS),
+                                   int(P), _typed(POS, "torch.int32", "POS"), _ptr(dX), int(lddx), _ptr(dWq),
+                                   _ptr(dWk), _ptr(workspace), int(ws_bytes), int(B), int(S), int(Hq), int(Hkv),
+                                   int(D), _stream(stream)), "lt_qknorm_rope_bwd")
+
+
+def lt_embed_fwd(ids, W, ldw, scale, Y, ldy, T, H, V, stream=None):
+    _check(_lib.lt_embed_fwd(_typed(ids, "torch.int64", "ids"), _ptr(W), int(ldw), float(scale), _ptr(Y), int(ldy),
+                             int(T), int(H), int(V), _stream(stream)), "lt_embed_fwd")
+
+
+def lt_embed_bwd_workspace_size(T, H, V):
+    return int(_lib.lt_embed_bwd_workspace_size(int(T), int(H), int(V)))
+
+
+def lt_embed_bwd(ids, dY, lddy, scale, accumulate, dW, lddw, workspace, ws_bytes, T, H, V, stream=None):
+    _check(_lib.lt_embed_bwd(_typed(ids, "torch.int64", "ids"), _ptr(dY), int(lddy), float(scale), int(accumulate),
+                             _ptr(dW), int(lddw), _ptr(workspace), int(ws_bytes), int(T), int(H), int(V),
+                             _stream(stream)), "lt_embed_bwd")
 
 
 def declared_functions():

@@ -1,0 +1,150 @@
+"""GPU parity of lt_qknorm_rope_fwd / lt_qknorm_rope_bwd against the float64 oracle, element by element.
+
+Bounds: the arithmetic is FP32 with one FP16 rounding, h = 2^-11 of the value (2^-25 below
+the normal range).  r: 2^-23 (D + 8) of itself.  y: with u = w x r,
+|u1 cos| + |u2 sin| times 2^-23 (D + 12), the angles' cosines being off by 2^-23 more.
+dx: r |w g| + |x| r^3 mean |g w x| times 2^-23 (D + 16).  dw: FP32 sums of n terms,
+2^-23 (n + D + 16) sum |g x r|.
+"""
+
+import numpy as np
+import pytest
+
+import oracle
+
+pytestmark = pytest.mark.gpu
+
+H, SUB, F = 2.0 ** -11, 2.0 ** -25, 2.0 ** -23
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a ROCm device"
+    from paper_2606_10415_amd import lt
+    return torch, lt
+
+
+def f16(rng, *shape, std=1.0, mean=0.0):
+    return (rng.standard_normal(shape, dtype=np.float32) * std + mean).astype(np.float16)
+
+
+def rot_abs(a, c, s):
+    h = a.shape[-1] // 2
+    return np.concatenate([a[..., :h] * c + a[..., h:] * s, a[..., h:] * c + a[..., :h] * s], axis=-1)
+
+
+@pytest.mark.parametrize("B,S,Hq,Hkv,D,P,std,pad,inplace", [
+    (1, 1, 1, 1, 16, 1, 1.0, 0, False),
+    (2, 3, 3, 1, 32, 50, 1.0, 8, True),
+    (1, 37, 5, 5, 48, 40, 2.0, 0, False),
+    (3, 65, 8, 2, 64, 4096, 1.0, 0, True),
+    (1, 130, 7, 1, 80, 131072, 1.0, 24, False),
+    (2, 77, 12, 4, 96, 100, 0.01, 0, False),
+    (1, 1500, 40, 8, 128, 4096, 2.0, 8, True),
+    (1, 50, 64, 8, 128, 64, 100.0, 0, False),
+    (1, 513, 4, 4, 256, 32768, 1.0, 0, True),
+    (1, 5001, 2, 1, 64, 5001, 1.0, 0, False),
+])
+@pytest.mark.parametrize("given", [True, False], ids=["positions", "in order"])
+def test_parity(env, B, S, Hq, Hkv, D, P, std, pad, inplace, given):
+    torch, lt = env
+    print("qknorm", B, S, Hq, Hkv, D, P, std, pad, inplace, given, flush=True)
+    rng = np.random.Generator(np.random.PCG64(31 + S + D))
+    if not given:
+        P = max(P, S)
+    T, n, base, eps = B * S, Hq + Hkv, 500000.0, 1e-6
+    W = (Hq + 2 * Hkv) * D + pad
+    qkv = f16(rng, T + 1, W, std=std)
+    if T > 2:
+        qkv[1, :n * D] = 0                            # a row of zeros: r = eps^(-1/2)
+    dy = f16(rng, T + 1, n * D + pad)
+    wq, wk = f16(rng, D, std=0.1, mean=1.0), f16(rng, D, std=0.1, mean=1.0)
+    pos = rng.integers(0, P, size=T).astype(np.int32) if given else np.tile(np.arange(S, dtype=np.int32), B)
+    cu = lambda a: torch.from_numpy(a).cuda()
+    X, dY, Wq, Wk = cu(qkv), cu(dy), cu(wq), cu(wk)
+    POS = cu(pos) if given else None
+    CS = torch.empty(P, D // 2, 2, device="cuda")
+    lt.lt_rope_table(CS, P, D, base)
+    Y = torch.full((T + 1, n * D + pad), 9.0, dtype=torch.float16, device="cuda")
+    RSTD = torch.full((T + 1, n), 9.0, device="cuda")
+    lt.lt_qknorm_rope_fwd(X, W, Wq, Wk, CS, P, POS, Y, n * D + pad, RSTD, B, S, Hq, Hkv, D, eps)
+    ws_n = lt.lt_qknorm_rope_bwd_workspace_size(B, S, Hq, Hkv, D)
+    ws = torch.full((ws_n + 256,), 0xff, dtype=torch.uint8, device="cuda")
+    dX = dY if inplace else torch.full((T + 1, n * D + pad), 9.0, dtype=torch.float16, device="cuda")
+    dwq, dwk = (torch.full((D,), float("nan"), dtype=torch.float16, device="cuda") for _ in range(2))
+    lt.lt_qknorm_rope_bwd(dY, n * D + pad, X, W, Wq, Wk, RSTD, CS, P, POS, dX, n * D + pad, dwq, dwk, ws, ws_n, B, S,
+                          Hq, Hkv, D)
+    Yi = X.clone()                                    # forward in place
+    Ri = torch.empty_like(RSTD)
+    lt.lt_qknorm_rope_fwd(Yi, W, Wq, Wk, CS, P, POS, Yi, W, Ri, B, S, Hq, Hkv, D, eps)
+    torch.cuda.synchronize()
+    assert bool((ws[ws_n:] == 0xff).all())
+    assert np.array_equal(X.cpu().numpy().view(np.uint16), qkv.view(np.uint16))
+    y, dx, rstd = Y.cpu().numpy(), dX.cpu().numpy(), RSTD.cpu().numpy()
+    yi = Yi.cpu().numpy()
+    assert np.array_equal(yi[:T, :n * D].view(np.uint16), y[:T, :n * D].view(np.uint16))
+    assert np.array_equal(yi[:, n * D:].view(np.uint16), qkv[:, n * D:].view(np.uint16))
+    assert np.all(y[T] == 9.0) and np.all(y[:, n * D:] == 9.0) and np.all(rstd[T] == 9.0)
+    if inplace:
+        assert np.array_equal(dx[T], dy[T]) and np.array_equal(dx[:, n * D:], dy[:, n * D:])
+    else:
+        assert np.all(dx[T] == 9.0) and np.all(dx[:, n * D:] == 9.0)
+
+    x = qkv[:T, :n * D].reshape(T, n, D).astype(np.float64)
+    g = dy[:T, :n * D].reshape(T, n, D).astype(np.float64)
+    ry, rr, rdx, rdwq, rdwk = oracle.qknorm_rope(x, wq, wk, Hq, pos, base, eps, g)
+    a = pos[:, None] * base ** (-2.0 * np.arange(D // 2) / D)
+    c, s = abs(np.cos(a))[:, None, :] + F, abs(np.sin(a))[:, None, :] + F
+    w = np.where((np.arange(n) < Hq)[:, None], wq.astype(np.float64), wk.astype(np.float64))
+    assert np.all(abs(rstd[:T] / rr - 1) <= F * (D + 8))
+    ty = F * (D + 12) * rot_abs(abs(w * x * rr[..., None]), c, s) + H * abs(ry) + SUB
+    assert np.all(abs(y[:T, :n * D].reshape(T, n, D) - ry) <= ty)
+    ag = rot_abs(abs(g), c, s)
+    mag = rr[..., None] * abs(w) * ag + abs(x) * (rr ** 3)[..., None] * np.mean(ag * abs(w * x), 2, keepdims=True)
+    assert np.all(abs(dx[:T, :n * D].reshape(T, n, D) - rdx) <= F * (D + 16) * mag + H * abs(rdx) + SUB)
+    terms = ag * abs(x) * rr[..., None]
+    for got, ref, sl in ((dwq, rdwq, slice(0, Hq)), (dwk, rdwk, slice(Hq, n))):
+        cnt = T * (sl.stop - sl.start)
+        tol = F * (cnt + D + 16) * terms[:, sl].sum((0, 1)) + H * abs(ref) + SUB
+        got = got.cpu().numpy().astype(np.float64)
+        fits = abs(ref) + tol < 65504                 # a sum beyond FP16 is infinite, as it should be
+        assert np.all(abs(got - ref)[fits] <= tol[fits])
+
+
+def test_position_outside_the_table_is_nan(env):
+    torch, lt = env
+    rng = np.random.Generator(np.random.PCG64(3))
+    S, D, P = 6, 64, 4
+    X = torch.from_numpy(f16(rng, S, 3 * D)).cuda()
+    w = torch.ones(D, dtype=torch.float16, device="cuda")
+    CS = torch.empty(P, D // 2, 2, device="cuda")
+    lt.lt_rope_table(CS, P, D, 10000.0)
+    POS = torch.tensor([0, 3, 4, -1, 2 ** 31 - 1, 1], dtype=torch.int32, device="cuda")
+    Y, R = torch.empty(S, 2 * D, dtype=torch.float16, device="cuda"), torch.empty(S, 2, device="cuda")
+    lt.lt_qknorm_rope_fwd(X, 3 * D, w, w, CS, P, POS, Y, 2 * D, R, 1, S, 1, 1, D, 1e-6)
+    bad = torch.isnan(Y).all(1).cpu().tolist()
+    assert bad == [False, False, True, True, True, False]
+    assert bool(torch.isfinite(Y[[0, 1, 5]]).all()) and bool(torch.isfinite(R).all())
+
+
+def test_results_repeat_bitwise(env):
+    torch, lt = env
+    rng = np.random.Generator(np.random.PCG64(4))
+    B, S, Hq, Hkv, D = 1, 3000, 8, 2, 128
+    n = Hq + Hkv
+    X, dY = (torch.from_numpy(f16(rng, S, n * D)).cuda() for _ in range(2))
+    w = torch.ones(D, dtype=torch.float16, device="cuda")
+    CS = torch.empty(S, D // 2, 2, device="cuda")
+    lt.lt_rope_table(CS, S, D, 10000.0)
+    outs = []
+    for _ in range(2):
+        Y, R = torch.empty_like(X), torch.empty(S, n, device="cuda")
+        dX, dq, dk = torch.empty_like(X), torch.empty_like(w), torch.empty_like(w)
+        wn = lt.lt_qknorm_rope_bwd_workspace_size(B, S, Hq, Hkv, D)
+        ws = torch.empty(wn, dtype=torch.uint8, device="cuda")
+        lt.lt_qknorm_rope_fwd(X, n * D, w, w, CS, S, None, Y, n * D, R, B, S, Hq, Hkv, D, 1e-6)
+        lt.lt_qknorm_rope_bwd(dY, n * D, X, n * D, w, w, R, CS, S, None, dX, n * D, dq, dk, ws, wn, B, S, Hq, Hkv, D)
+        outs.append([t.cpu().numpy().view(np.uint8) for t in (Y, R, dX, dq, dk)])
+    for a, b in zip(*outs):
+        assert np.array_equal(a, b)
