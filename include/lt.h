@@ -539,8 +539,9 @@ lt_status lt_qknorm_rope_bwd(const lt_half* dY, int64_t lddy, const lt_half* X,
  * 0 .. V - 1 (-1, say) is padding: a row of zeros.  One rounding per output.
  * T == 0 is a no-op.  Errors: LT_ERR_INVALID_ARG for NULL pointers, T < 0, H or
  * V < 1, strides below H, scale not finite; LT_ERR_UNSUPPORTED for H not a
- * multiple of 8 or above 65536, strides not multiples of 8, T or V >= 2^30,
- * W or Y not 16-byte, ids not 8-byte aligned.
+ * multiple of 8 or above 65536, strides not multiples of 8, T >= 2^24,
+ * V >= 2^25 or ceil(T / 16) ceil(H / 512) + V / 4 >= 2^24 - 1, W or Y not 16-byte,
+ * ids not 8-byte aligned.
  */
 lt_status lt_embed_fwd(const int64_t* ids, const lt_half* W, int64_t ldw,
                        float scale, lt_half* Y, int64_t ldy, int64_t T,

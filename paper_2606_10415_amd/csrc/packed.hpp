@@ -131,6 +131,35 @@ hipError_t qknorm_bwd_launch(const QkNormArgs& a, const lt_half* dY, int64_t ldd
                              int64_t lddx, lt_half* dWq, lt_half* dWk, float* part, hipStream_t s);
 
 // ---------------------------------------------------------------- embedding
+// Gradient: the tokens are sorted by row (stable); a row of more than kEmbedPart
+// tokens is summed in pieces of so many.
+constexpr int kEmbedPart = 16;
+// rows of the table per sorting workgroup: a power of two that gives 128 to 256
+// workgroups where the table has the rows for it
+inline int embed_sort_rows(int64_t V) {
+  int r = 32;
+  while (r < 1024 && V / (2 * r) >= 128) r *= 2;
+  return r;
+}
+inline int64_t embed_parts(int64_t T) { return (T + kEmbedPart - 1) / kEmbedPart; }
+// Workspace: start [V + 1] (first sorted position of a row), tokens [T] in
+// sorted order, two FP32 partial rows per kEmbedPart positions, each 256-byte
+// aligned.
+struct EmbedWs {
+  size_t tokens, part, total;
+};
+inline EmbedWs embed_bwd_ws(int64_t T, int64_t H, int64_t V) {
+  EmbedWs w;
+  w.tokens = align256((size_t)(V + 1) * sizeof(int32_t));
+  w.part = w.tokens + align256((size_t)T * sizeof(int32_t));
+  w.total = w.part + align256((size_t)2 * embed_parts(T) * H * sizeof(float));
+  return w;
+}
+// workgroups of the largest launch (256 threads each, below 2^32 threads)
+inline bool embed_fits(int64_t T, int64_t H, int64_t V) {
+  return T < (int64_t)1 << 24 && V < (int64_t)1 << 25 &&
+         embed_parts(T) * ((H + 511) / 512) + V / 4 + 1 < (int64_t)1 << 24;
+}
 struct EmbedBwdArgs {
   const int64_t* ids;
   const lt_half* dY;
@@ -140,9 +169,10 @@ struct EmbedBwdArgs {
   lt_half* dW;
   int64_t lddw;
   int64_t T, H, V;
-  char* ws;
+  int32_t* start;         // workspace, see EmbedWs
+  int32_t* tokens;
+  float* part;
 };
-inline size_t embed_bwd_ws_bytes(int64_t, int64_t, int64_t) { return 256; }
 hipError_t embed_fwd_launch(const int64_t* ids, const lt_half* W, int64_t ldw, float scale, lt_half* Y, int64_t ldy,
                             int64_t T, int64_t H, int64_t V, hipStream_t s);
 hipError_t embed_bwd_launch(const EmbedBwdArgs& a, hipStream_t s);

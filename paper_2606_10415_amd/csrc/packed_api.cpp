@@ -102,7 +102,7 @@ lt_status check_embed(const int64_t* ids, const void* A, int64_t lda, const void
   if (!std::isfinite(scale)) return fail(LT_ERR_INVALID_ARG, "scale must be finite");
   if ((H & 7) || H > 65536) return fail(LT_ERR_UNSUPPORTED, "H must be a multiple of 8 and <= 65536");
   if ((lda | ldc) & 7) return fail(LT_ERR_UNSUPPORTED, "row strides must be multiples of 8 elements");
-  if (T >= (int64_t)1 << 30 || V >= (int64_t)1 << 30) return fail(LT_ERR_UNSUPPORTED, "T and V must be < 2^30");
+  if (!lt::embed_fits(T, H, V)) return fail(LT_ERR_UNSUPPORTED, "too many tokens, columns or rows for one launch");
   if (!aligned(A, 16) || !aligned(C, 16)) return fail(LT_ERR_UNSUPPORTED, "rows must be 16-byte aligned");
   if (!aligned(ids, 8)) return fail(LT_ERR_UNSUPPORTED, "ids must be 8-byte aligned");
   return LT_OK;
@@ -224,8 +224,8 @@ lt_status lt_embed_fwd(const int64_t* ids, const lt_half* W, int64_t ldw, float 
 }
 
 size_t lt_embed_bwd_workspace_size(int64_t T, int64_t H, int64_t V) {
-  if (T < 0 || H < 1 || V < 1 || (H & 7) || H > 65536 || T >= (int64_t)1 << 30 || V >= (int64_t)1 << 30) return 0;
-  return lt::embed_bwd_ws_bytes(T, H, V);
+  if (T < 0 || H < 1 || V < 1 || (H & 7) || H > 65536 || !lt::embed_fits(T, H, V)) return 0;
+  return lt::embed_bwd_ws(T, H, V).total;
 }
 
 lt_status lt_embed_bwd(const int64_t* ids, const lt_half* dY, int64_t lddy, float scale, int accumulate, lt_half* dW,
@@ -235,9 +235,23 @@ lt_status lt_embed_bwd(const int64_t* ids, const lt_half* dY, int64_t lddy, floa
   lt_status st = check_embed(ids, T > 0 ? dY : dW, T > 0 ? lddy : H, dW, lddw, scale, T, H, V);
   if (st != LT_OK) return st;
   if (accumulate != 0 && accumulate != 1) return fail(LT_ERR_INVALID_ARG, "accumulate must be 0 or 1");
-  if ((st = check_workspace(workspace, ws_bytes, lt::embed_bwd_ws_bytes(T, H, V))) != LT_OK) return st;
+  const lt::EmbedWs w = lt::embed_bwd_ws(T, H, V);
+  if ((st = check_workspace(workspace, ws_bytes, w.total)) != LT_OK) return st;
   if (T == 0 && accumulate) return ok();
-  lt::EmbedBwdArgs a{ids, dY, lddy, scale, accumulate, dW, lddw, T, H, V, static_cast<char*>(workspace)};
+  char* ws = static_cast<char*>(workspace);
+  lt::EmbedBwdArgs a{ids,
+                     dY,
+                     lddy,
+                     scale,
+                     accumulate,
+                     dW,
+                     lddw,
+                     T,
+                     H,
+                     V,
+                     reinterpret_cast<int32_t*>(ws),
+                     reinterpret_cast<int32_t*>(ws + w.tokens),
+                     reinterpret_cast<float*>(ws + w.part)};
   return from_hip(lt::embed_bwd_launch(a, reinterpret_cast<hipStream_t>(stream)), "embed_bwd launch");
 }
 

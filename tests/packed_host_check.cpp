@@ -83,7 +83,11 @@ hipError_t embed_fwd_launch(const int64_t*, const lt_half*, int64_t, float, lt_h
 }
 hipError_t embed_bwd_launch(const EmbedBwdArgs& a, hipStream_t) {
   ++g_launches;
-  inside(a.ws, embed_bwd_ws_bytes(a.T, a.H, a.V), 0, "embedding workspace");
+  uintptr_t at = inside(a.start, (size_t)(a.V + 1) * 4, 0, "row starts");
+  at = inside(a.tokens, (size_t)a.T * 4, at, "sorted tokens");
+  inside(a.part, (size_t)2 * ((a.T + kEmbedPart - 1) / kEmbedPart) * a.H * 4, at, "partial rows");
+  const int r = embed_sort_rows(a.V);
+  CHECK(r >= 32 && r <= 1024 && (r & (r - 1)) == 0, "rows per sorting workgroup %d", r);
   return hipErrorNoDevice;
 }
 }  // namespace lt
