@@ -4,7 +4,6 @@
 //   s = scale q.k;  capped: s = cap tanh(s / cap);  biased: s -= slope |i - j|
 //   query i sees the keys of one interval
 //
-// The kernels keep modified scores in base-2 units (z = s log2 e).
 #pragma once
 
 #include "packed.hpp"
@@ -27,19 +26,50 @@ __device__ __forceinline__ void row_interval(const ScoreMod& m, int causal, int 
   if (lo >= hi) lo = hi = 0;
 }
 
-// The cap in base-2 units: z = C tanh(s / cap), C = cap log2 e, s the raw
-// product.  With u = 1 / (1 + e^(2 s scale / cap)): tanh = 1 - 2 u and
-// 1 - tanh^2 = 4 u (1 - u).  The absolute error is a few 2^-24 C, so that a
-// probability is off by less than an FP16 half step up to caps of 1000.
-struct Cap {
-  float k2, c, c2;
-  __device__ __forceinline__ Cap(float cap, float scale)
-      : k2(cap > 0.f ? 2.f * scale / cap * kModLog2e : 0.f), c(cap * kModLog2e), c2(-2.f * cap * kModLog2e) {}
-  __device__ __forceinline__ float u(float s) const {
-    return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * k2));
+// Stored scores.  The kernels keep a score as t with z = c t + const in base-2
+// units, so that a probability is one FMA and one exp2 from it:
+//   * without a cap t = q.k and c = scale log2 e;
+//   * with one, tanh(x) = 1 - 2 u, u = 1 / (1 + e^(2 x)), x = scale q.k / cap: t = -u,
+//     c = 2 cap log2 e, const = cap log2 e, and 1 - tanh^2 = 4 u (1 - u).  The
+//     absolute error of z is a few 2^-24 c, so that a probability is off by less than
+//     an FP16 half step up to caps of 1000.
+// The bias in units of t is slope' |i - j|, slope' = slope log2 e / c.  Without a
+// cap it enters as the initial value of the product's FP32 accumulator (its
+// rounding there is relative to the bias: only keys whose probability the bias has
+// made negligible see it).
+template <bool CAP>
+struct Score {
+  float c, k2, off;        // t -> base-2 units, product -> exponent of u, const
+  __device__ __forceinline__ Score(const ScoreMod& m, float scale)
+      : c(CAP ? 2.f * m.cap * kModLog2e : scale * kModLog2e),
+        k2(CAP ? 2.f * scale / m.cap * kModLog2e : 0.f),
+        off(CAP ? m.cap * kModLog2e : 0.f) {}
+  __device__ __forceinline__ float t(float s) const {
+    if constexpr (CAP) return __builtin_amdgcn_rcpf(-1.f - fast_exp2(s * k2));
+    return s;
   }
-  __device__ __forceinline__ float z(float u) const { return fmaf(c2, u, c); }
 };
+
+// Values -slope' |d0 + n| of a 32-wide accumulator column, n = 8 (r / 4) + r % 4, r < 16,
+// step by step of kb (32 more).  `side`: every d0 + n of the wave has that sign (+1, -1),
+// or 0: mixed.  With a sign the value is linear in n: one add of a scalar each.
+template <int N>
+__device__ __forceinline__ void bias_init(f32x16 (&acc)[N], float slope, float d0, int side) {
+  if (side != 0) {
+    const float m = side > 0 ? -slope : slope;     // wave-uniform
+    const float base = m * d0;
+#pragma unroll
+    for (int kb = 0; kb < N; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[kb][r] = fmaf(m, (float)(kb * 32 + 8 * (r >> 2) + (r & 3)), base);
+  } else {
+#pragma unroll
+    for (int kb = 0; kb < N; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        acc[kb][r] = -slope * fabsf(d0 + (float)(kb * 32 + 8 * (r >> 2) + (r & 3)));
+  }
+}
 
 __device__ __forceinline__ int wave_min32(int v) {   // over lane % 32
 #pragma unroll

@@ -9,7 +9,8 @@
 // Kernels, none with an atomic:
 //   1. attn_mod_rows: D_i and the base-2 LSE of every query and head; the
 //      clamped interval of every query and the hull of every 32 queries'
-//      intervals, which the other passes select their blocks by.  HBM-bound.
+//      intervals, which the other passes select their blocks by.  attn_mod_delta:
+//      D_i again, in FP32, where the FP16 O is too coarse for it.
 //   2. attn_mod_dkdv: key-major.  One workgroup per (batch, kv head, 256-key
 //      tile); each of 8 waves owns 32 keys, with their K fragments and the dK, dV
 //      accumulators in registers.  It lists the 64-query blocks that see some of
@@ -59,58 +60,274 @@ __device__ __forceinline__ int64_t ds_block(int qg, int kg, int n32, int causal)
 }
 
 // ------------------------------------------------------------ 1: row terms, intervals, hulls
-// Workgroups 0 .. n_term - 1: D / 8 lanes per row (one 16-byte chunk each),
-// consecutive queries of one (batch, head); the row's lanes add in a fixed order.
-// The others: 256 queries of one batch row, a lane each.
-template <int D>
-__global__ void __launch_bounds__(256)
-attn_mod_rows_kernel(const lt_half* __restrict__ O, const lt_half* __restrict__ dO, int64_t o_stride,
-                     const float* __restrict__ LSE, float* __restrict__ lse2, float* __restrict__ delta,
-                     const ScoreMod mod, int32_t* __restrict__ rows, QueryHull* __restrict__ hulls,
-                     unsigned n_term, int B, int S, int Hq, int causal) {
-  if (blockIdx.x >= n_term) {
-    const int n_sb = (S + 255) / 256;
-    const int b = (blockIdx.x - n_term) / n_sb;
-    const int q = ((blockIdx.x - n_term) % n_sb) * 256 + threadIdx.x;
-    int lo, hi;
-    row_interval(mod, causal, b, S, q, lo, hi);
-    if (q < S) {
-      rows[(int64_t)b * S + q] = lo;
-      rows[(int64_t)(B + b) * S + q] = hi;
-    }
-    // both halves of the wave are a group of 32
-    const bool some = lo < hi;
-    QueryHull h;
-    h.lo = wave_min32(some ? lo : 0x7fffffff);
-    h.hi = wave_max32(some ? hi : 0);
-    h.all_lo = wave_max32(q >= S ? 0 : some ? lo : 0x7fffffff);
-    h.all_hi = wave_min32(q >= S ? 0x7fffffff : some ? hi : 0);
-    if ((threadIdx.x & 31) == 0 && q < S) hulls[(int64_t)b * ((S + 31) / 32) + q / 32] = h;
-    return;
-  }
-  constexpr int CPR = D / 8;
-  constexpr int RPB = 256 / CPR;                   // rows per workgroup
-  const int n_sb = (S + RPB - 1) / RPB;
-  const int bh = blockIdx.x / n_sb;
-  const int q = (blockIdx.x % n_sb) * RPB + (int)threadIdx.x / CPR;
-  const int c = threadIdx.x % CPR;
-  const int b = bh / Hq;
-  const int h = bh % Hq;
-  float part = 0.f;
+// D_i = rowsum(dO_i * O_i) = sum_j P_ij dP_ij.  Formed from the FP16 O, D is off by
+// about 2^-12 |dO| |O|.  Where a softmax is spread over many keys |O| is small
+// against |v| and that drowns in the rounding of dS; where it rests on a few keys
+// dP - D cancels and it does not: with scores of standard deviation 9 it took
+// the error of dQ and dK from 2.9e-4 to 5.5e-4 of their norm.  So queries whose O
+// is not small are marked sharp, and attn_mod_delta forms their D again: those with
+// |O|^2 > kFlat |v|^2 (v at the same position) in groups of 32 that are so on average, and
+// elsewhere those with four times that.  At kFlat the D of the FP16 O adds 0.7e-4.
+constexpr int kTile = kSharpTile;
+constexpr float kFlat = 1.f / 16.f;
+
+// Intervals and hulls of the 256 queries of block blk of the batch rows, a lane each.
+__device__ __forceinline__ void rows_and_hulls(const AttnModBwdArgs& a, int blk) {
+  const int B = a.sh.B, S = a.sh.S, n_sb = (S + 255) / 256;
+  const int b = blk / n_sb, q = (blk % n_sb) * 256 + threadIdx.x;
+  int lo, hi;
+  row_interval(a.mod, a.sh.causal, b, S, q, lo, hi);
   if (q < S) {
-    const int64_t off = ((int64_t)b * S + q) * o_stride + (int64_t)h * D + c * 8;
-    const half8 x = as_half8(ld16(dO + off));
-    const half8 y = as_half8(ld16(O + off));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) part = fmaf((float)x[e], (float)y[e], part);
+    a.rows[(int64_t)b * S + q] = lo;
+    a.rows[(int64_t)(B + b) * S + q] = hi;
   }
+  // both halves of the wave are a group of 32
+  const bool some = lo < hi;
+  QueryHull h;
+  h.lo = wave_min32(some ? lo : 0x7fffffff);
+  h.hi = wave_max32(some ? hi : 0);
+  h.all_lo = wave_max32(q >= S ? 0 : some ? lo : 0x7fffffff);
+  h.all_hi = wave_min32(q >= S ? 0x7fffffff : some ? hi : 0);
+  if ((threadIdx.x & 31) == 0 && q < S) a.hulls[(int64_t)b * ((S + 31) / 32) + q / 32] = h;
+}
+
+// Workgroups 0 .. n_tile - 1: 128 queries of one head, D / 8 lanes to a row (whole
+// rows, coalesced).  The others: intervals and hulls.  HBM-bound.
+template <int D, bool CAP>
+__global__ void __launch_bounds__(256)
+attn_mod_rows_kernel(const AttnModBwdArgs a, unsigned n_tile) {
+  __shared__ float2 norm_s[kTile];                 // |O|^2 - kFlat |v|^2, |v|^2
+  const int B = a.sh.B, S = a.sh.S, Hq = a.sh.Hq;
+  if (blockIdx.x >= n_tile) return rows_and_hulls(a, blockIdx.x - n_tile);
+  constexpr int CPR = D / 8, RPI = 256 / CPR;      // lanes per row, rows per pass
+  const int bh = blockIdx.x % (B * Hq);
+  const int q0 = (int)(blockIdx.x / (B * Hq)) * kTile;
+  const int b = bh / Hq, h = bh % Hq, kvh = h / (Hq / a.sh.Hkv);
+  const int c8 = (threadIdx.x % CPR) * 8;
+  const Score<CAP> sc(a.mod, a.sh.scale);
 #pragma unroll
-  for (int m = CPR / 2; m >= 1; m >>= 1) part += __shfl_xor(part, m);
-  if (q < S && c == 0) {
-    const int64_t ri = (int64_t)bh * S + q;
-    delta[ri] = part;
-    lse2[ri] = LSE[ri] * kModLog2e;
+  for (int it = 0; it < kTile / RPI; ++it) {
+    const int r = it * RPI + threadIdx.x / CPR, q = q0 + r;
+    const u32x4 zero = {0, 0, 0, 0};
+    const int64_t row = (int64_t)b * S + q, off = row * a.o_stride + (int64_t)h * D + c8;
+    const half8 x = as_half8(q < S ? ld16(a.dO + off) : zero);
+    const half8 o = as_half8(q < S ? ld16(a.O + off) : zero);
+    const half8 v = as_half8(q < S ? ld16(a.V + row * a.kv_stride + (int64_t)kvh * D + c8) : zero);
+    float d = 0.f, o2 = 0.f, v2 = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      d = fmaf((float)x[e], (float)o[e], d);
+      o2 = fmaf((float)o[e], (float)o[e], o2);
+      v2 = fmaf((float)v[e], (float)v[e], v2);
+    }
+#pragma unroll
+    for (int m = CPR / 2; m >= 1; m >>= 1) {
+      d += __shfl_xor(d, m);
+      o2 += __shfl_xor(o2, m);
+      v2 += __shfl_xor(v2, m);
+    }
+    if (c8 == 0) norm_s[r] = make_float2(o2 - kFlat * v2, v2);
+    if (c8 == 0 && q < S) {
+      const int64_t ri = (int64_t)bh * S + q;
+      a.delta[ri] = d;
+      a.lse2[ri] = a.LSE[ri] * kModLog2e - sc.off;
+    }
   }
+  __syncthreads();
+  if (threadIdx.x < kTile) {                       // whole waves
+    const float2 n = norm_s[threadIdx.x];
+    float sum = n.x;
+#pragma unroll
+    for (int m = 16; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
+    const uint64_t bal = __builtin_amdgcn_ballot_w64(sum <= 0.f ? !(n.x <= 3.f * kFlat * n.y) : !(n.x <= 0.f));
+    if ((threadIdx.x & 31) == 0)
+      a.sharp[((int64_t)bh * ((S + kTile - 1) / kTile) + q0 / kTile) * (kTile / 32) + threadIdx.x / 32] =
+          (uint32_t)(threadIdx.x & 32 ? bal >> 32 : bal);
+  }
+}
+
+// D of the sharp queries in FP32 from S and dP, as the forward forms O: two
+// products.  One workgroup per (128 queries, or 64 with QSPLIT = 2 where the two waves of
+// a query group take one 32-key block of a slice each) of one head; they walk the keys
+// of their sharp queries.  `all` (short sequences, where another launch costs more than
+// these products): every query is taken, the base-2 LSE is written too, and the
+// workgroups from n_tile on do the intervals and hulls, in place of attn_mod_rows.
+constexpr int NWD = 4;            // waves
+constexpr int BKD = 64;           // keys per slice
+
+template <int D, int QSPLIT, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(NWD * 64, 2)
+attn_mod_delta_kernel(const AttnModBwdArgs a, int all, unsigned n_tile) {
+  using RT = RowTile<D, NWD>;
+  constexpr int KK = D / 16;
+  constexpr int NQG = NWD / QSPLIT;                // query groups of 32
+  constexpr int BQW = NQG * 32;                    // queries per workgroup
+  constexpr int KBW = BKD / 32 / QSPLIT;           // 32-key blocks per slice and wave
+  constexpr int TILE = BKD * RT::ROWB, STAGE = 2 * TILE;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  __shared__ int hull_s[2][NWD];
+
+  const int B = a.sh.B, S = a.sh.S, Hq = a.sh.Hq, Hkv = a.sh.Hkv, causal = a.sh.causal;
+  if (blockIdx.x >= n_tile) return rows_and_hulls(a, blockIdx.x - n_tile);
+  const int n_qt = (S + BQW - 1) / BQW;
+  const int qt = causal ? n_qt - 1 - (int)(blockIdx.x / (B * Hq)) : (int)(blockIdx.x / (B * Hq));
+  int b, h;
+  query_head(blockIdx.x % (B * Hq), B, Hq, Hkv, b, h);
+  const uint32_t* marks = a.sharp + ((int64_t)b * Hq + h) * ((S + kTile - 1) / kTile) * (kTile / 32) + qt * NQG;
+  if (!all) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int w = 0; w < NQG; ++w) any |= marks[w];
+    if (!any) return;
+  }
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lrow = lane & 31, g = lane >> 5;
+  const int qg = wave % NQG, kpart = wave / NQG;
+  const int kvh = h / (Hq / Hkv);
+  const int qw0 = qt * BQW + qg * 32;
+  const int myq = qw0 + lrow;                      // query owned by this lane
+  const lt_half* Kp = a.K + (int64_t)b * S * a.kv_stride + (int64_t)kvh * D;
+  const lt_half* Vp = a.V + (int64_t)b * S * a.kv_stride + (int64_t)kvh * D;
+  const int64_t row = (int64_t)b * S + (myq < S ? myq : 0), ri = ((int64_t)b * Hq + h) * S + myq;
+
+  const Score<CAP> sc(a.mod, a.sh.scale);
+  const float lse2 = myq < S ? (all ? a.LSE[ri] * kModLog2e - sc.off : a.lse2[ri]) : 0.f;
+  if (all && myq < S && g == 0 && kpart == 0) {
+    a.lse2[ri] = lse2;
+    a.delta[ri] = 0.f;                             // kept by queries that see nothing
+  }
+  int lo = 0, hi = 0;
+  if (all || (marks[qg] >> lrow & 1)) row_interval(a.mod, causal, b, S, myq, lo, hi);
+  const QueryHull wh = query_hull(lo, hi, myq < S);
+  if (lane == 0) {
+    hull_s[0][wave] = wh.lo;
+    hull_s[1][wave] = wh.hi;
+  }
+  __syncthreads();
+  int wg_lo = 0x7fffffff, wg_hi = 0;
+#pragma unroll
+  for (int w = 0; w < NWD; ++w) {
+    wg_lo = min(wg_lo, hull_s[0][w]);
+    wg_hi = max(wg_hi, hull_s[1][w]);
+  }
+  if (wg_lo >= wg_hi) return;                      // the same in every wave
+  const int kt0 = __builtin_amdgcn_readfirstlane(wg_lo / BKD);
+  const int kt1 = __builtin_amdgcn_readfirstlane((wg_hi + BKD - 1) / BKD);
+
+  // Q and dO fragments (B operands of S^T = K Q^T and dP^T = V dO^T)
+  half8 qf[KK], gf[KK];
+  {
+    const lt_half* qp = a.Q + row * a.q_stride + (int64_t)h * D + g * 8;
+    const lt_half* gp = a.dO + row * a.o_stride + (int64_t)h * D + g * 8;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      qf[kk] = as_half8(myq < S ? ld16(qp + kk * 16) : u32x4{0, 0, 0, 0});
+      gf[kk] = as_half8(myq < S ? ld16(gp + kk * 16) : u32x4{0, 0, 0, 0});
+    }
+  }
+  const float slope = BIAS ? a.mod.slopes[h] * kModLog2e / sc.c : 0.f;   // in units of the stored scores
+  uint32_t rlane[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) rlane[kk] = (uint32_t)RT::addr(lane & 31, kk * 2 + (lane >> 5));
+  auto stage_load = [&](int kt, int buf) {
+    char* st = smem + buf * STAGE;
+    const int key0 = kt * BKD;
+    RT::template dma<BKD>(st, Kp + (int64_t)key0 * a.kv_stride, a.kv_stride, S - key0, wave, lane);
+    RT::template dma<BKD>(st + TILE, Vp + (int64_t)key0 * a.kv_stride, a.kv_stride, S - key0, wave, lane);
+  };
+  stage_load(kt0, 0);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    loaded_here(qf[kk]);
+    loaded_here(gf[kk]);
+  }
+  float dex = 0.f;                                 // this lane's share of D
+  auto slice = [&](int kt, auto CUR_) {
+    constexpr int cur = decltype(CUR_)::value;
+    const char* st = smem + cur * STAGE;
+    if (kt + 1 < kt1) stage_load(kt + 1, cur ^ 1);
+    const int kb0 = QSPLIT > 1 ? kpart * 32 : 0;
+    const int key0 = kt * BKD + kb0;
+    if (key0 < wh.hi && key0 + KBW * 32 > wh.lo) {
+      f32x16 sacc[KBW], pacc[KBW];
+      const float d0 = (float)(key0 + 4 * g - myq);
+      // keys all from, or all up to, the wave's queries
+      const int side = key0 >= qw0 + 31 ? 1 : key0 + KBW * 32 - 1 <= qw0 ? -1 : 0;
+#pragma unroll
+      for (int kb = 0; kb < KBW; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sacc[kb][r] = 0.f;
+          pacc[kb][r] = 0.f;
+        }
+      if constexpr (BIAS && !CAP) bias_init(sacc, slope, d0, side);
+      auto rd = [&](int off, int kb, int kk) {
+        return as_half8(*reinterpret_cast<const u32x4*>(st + off + (kb0 + kb * 32) * RT::ROWB + rlane[kk]));
+      };
+      half8 kfr[2][KBW], vfr[2][KBW];
+#pragma unroll
+      for (int kb = 0; kb < KBW; ++kb) {
+        kfr[0][kb] = rd(0, kb, 0);
+        vfr[0][kb] = rd(TILE, kb, 0);
+      }
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        if (kk + 1 < KK) {
+#pragma unroll
+          for (int kb = 0; kb < KBW; ++kb) {
+            kfr[(kk + 1) & 1][kb] = rd(0, kb, kk + 1);
+            vfr[(kk + 1) & 1][kb] = rd(TILE, kb, kk + 1);
+          }
+        }
+#pragma unroll
+        for (int kb = 0; kb < KBW; ++kb) {
+          sacc[kb] = mfma32(kfr[kk & 1][kb], qf[kk], sacc[kb]);
+          pacc[kb] = mfma32(vfr[kk & 1][kb], gf[kk], pacc[kb]);
+        }
+      }
+      const bool full = key0 >= wh.all_lo && key0 + KBW * 32 <= wh.all_hi;      // wave-uniform
+#pragma unroll
+      for (int kb = 0; kb < KBW; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float t = sc.t(sacc[kb][r]);
+          if constexpr (CAP && BIAS) t = fmaf(-slope, fabsf(d0 + (float)(kb * 32 + 8 * (r >> 2) + (r & 3))), t);
+          sacc[kb][r] = fast_exp2(fmaf(t, sc.c, -lse2)) * pacc[kb][r];
+        }
+      if (!full) {
+#pragma unroll
+        for (int kb = 0; kb < KBW; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = key0 + kb * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
+            sacc[kb][r] = ((key >= lo) & (key < hi)) ? sacc[kb][r] : 0.f;
+          }
+      }
+#pragma unroll
+      for (int kb = 0; kb < KBW; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dex += sacc[kb][r];
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  for (int kt = kt0; kt < kt1; kt += 2) {
+    slice(kt, std::integral_constant<int, 0>{});
+    if (kt + 1 < kt1) slice(kt + 1, std::integral_constant<int, 1>{});
+  }
+  dex += __shfl_xor(dex, 32);
+  if constexpr (QSPLIT > 1) {
+    float* red = reinterpret_cast<float*>(smem);   // free after the loop's last barrier
+    if (kpart == 1) red[qg * 64 + lane] = dex;
+    __syncthreads();
+    if (kpart == 1) return;
+    dex += red[qg * 64 + lane];
+  }
+  if (myq < S && g == 0 && lo < hi) a.delta[ri] = dex;
 }
 
 // ------------------------------------------------------------ 2: dK/dV
@@ -231,8 +448,7 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
     }
 
   const float scale = a.sh.scale;
-  const float c = scale * kModLog2e;
-  const Cap cap(a.mod.cap, scale);
+  const Score<CAP> sc(a.mod, scale);
   // The (query head, listed block) pairs, head-major, in nsh contiguous shares.
   // Within a head the blocks run last to first: the key tiles of one kv head
   // (on one XCD by the workgroup order) then move in step under a causal mask,
@@ -294,7 +510,7 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
     const float* del_s = reinterpret_cast<const float*>(rowp + 256);
     const int* lo_s = reinterpret_cast<const int*>(rowp + 512);
     const int* hi_s = reinterpret_cast<const int*>(rowp + 768);
-    const float slope2 = BIAS ? a.mod.slopes[h] * kModLog2e : 0.f;
+    const float slope = BIAS ? a.mod.slopes[h] * kModLog2e / sc.c : 0.f;   // in units of the stored scores
 
     auto half = [&](int ih) {
       const int hq = KSPLIT > 1 ? kpart : ih;
@@ -305,12 +521,16 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
       const int all_lo = __builtin_amdgcn_readfirstlane(hv.z);
       const int all_hi = __builtin_amdgcn_readfirstlane(hv.w);
       if (qh < S && hlo < kw0 + 32 && hhi > kw0) { // wave-uniform
-        f32x16 sacc, pacc;
+        f32x16 sacc1[1], pacc;
+        f32x16& sacc = sacc1[0];
+        const float d0 = (float)(qh + 4 * g - mykey);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           sacc[r] = 0.f;
           pacc[r] = 0.f;
         }
+        // queries all from, or all up to, the wave's keys
+        if constexpr (BIAS && !CAP) bias_init(sacc1, slope, d0, qh >= kw0 + 31 ? 1 : qh + 31 <= kw0 ? -1 : 0);
         // fragments of step kk+1 are read before the MFMAs of step kk; the Q
         // and dO reads are a lane register plus a constant, the V read's address
         // is added right before it (kept there: holding eight V addresses
@@ -351,9 +571,8 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
           fv = nv;
         }
         __builtin_amdgcn_s_setprio(0);
-        // P = exp2(z - LSE2), dS = P (dP - D) (1 - tanh^2)
+        // P = exp2(c t - LSE2), dS = P (dP - D) (1 - tanh^2)
         float p[16], ds[16];
-        const float d0 = (float)(qh + 4 * g - mykey);
 #pragma unroll
         for (int rq = 0; rq < 4; ++rq) {
           const int ql0 = hq * 32 + 8 * rq + 4 * g;
@@ -364,18 +583,14 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int r = 4 * rq + e;
-            float z, w = 1.f;
+            float t = sc.t(sacc[r]);
+            ds[r] = pacc[r] - dv[e];
             if constexpr (CAP) {
-              const float u = cap.u(sacc[r]);
-              const float u4 = 4.f * u;
-              w = fmaf(-u4, u, u4);
-              z = cap.z(u) - lv[e];
-            } else {
-              z = fmaf(sacc[r], c, -lv[e]);
+              const float u4 = -4.f * t;               // 1 - tanh^2 = 4 u (1 - u), u = -t
+              ds[r] *= fmaf(u4, t, u4);
+              if constexpr (BIAS) t = fmaf(-slope, fabsf(d0 + (float)(8 * rq + e)), t);
             }
-            if constexpr (BIAS) z = fmaf(-slope2, fabsf(d0 + (float)(8 * rq + e)), z);
-            p[r] = fast_exp2(z);
-            ds[r] = CAP ? (pacc[r] - dv[e]) * w : pacc[r] - dv[e];
+            p[r] = fast_exp2(fmaf(t, sc.c, -lv[e]));
           }
         }
 #pragma unroll
@@ -732,16 +947,32 @@ attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
   }
 }
 
+constexpr int64_t kDeltaSlots = 512;  // workgroup slots: two per CU
+constexpr int kOnePassS = 512;        // longest sequence whose D is all formed from S and dP
 constexpr int64_t kDqHalfWgs = 128;   // 256-query workgroups up to which they hold 128
 
 template <int D, bool CAP, bool BIAS>
 hipError_t launch_bwd(const AttnModBwdArgs& a, hipStream_t s) {
   const AttnShape& sh = a.sh;
-  constexpr int rpb = 256 / (D / 8);
-  const unsigned n_term = (unsigned)((int64_t)sh.B * sh.Hq * ((sh.S + rpb - 1) / rpb));
   const unsigned n_rows = (unsigned)((int64_t)sh.B * ((sh.S + 255) / 256));
-  hipLaunchKernelGGL((attn_mod_rows_kernel<D>), dim3(n_term + n_rows), dim3(256), 0, s, a.O, a.dO, a.o_stride, a.LSE,
-                     a.lse2, a.delta, a.mod, a.rows, a.hulls, n_term, sh.B, sh.S, sh.Hq, sh.causal);
+  const int64_t n_tile = (int64_t)((sh.S + kTile - 1) / kTile) * sh.B * sh.Hq;
+  const int64_t n_tile64 = (int64_t)((sh.S + 63) / 64) * sh.B * sh.Hq;
+  if (sh.S <= kOnePassS && n_tile <= kDeltaSlots) {
+    hipLaunchKernelGGL((attn_mod_delta_kernel<D, 2, CAP, BIAS>), dim3((unsigned)n_tile64 + n_rows), dim3(NWD * 64), 0, s,
+                       a, 1, (unsigned)n_tile64);
+  } else {
+    hipLaunchKernelGGL((attn_mod_rows_kernel<D, CAP>), dim3((unsigned)n_tile + n_rows), dim3(256), 0, s, a,
+                       (unsigned)n_tile);
+    hipError_t er = hipGetLastError();
+    if (er != hipSuccess) return er;
+    // 64-query tiles where 128-query ones would not fill the CUs twice
+    if (n_tile > kDeltaSlots)
+      hipLaunchKernelGGL((attn_mod_delta_kernel<D, 1, CAP, BIAS>), dim3((unsigned)n_tile), dim3(NWD * 64), 0, s, a, 0,
+                         (unsigned)n_tile);
+    else
+      hipLaunchKernelGGL((attn_mod_delta_kernel<D, 2, CAP, BIAS>), dim3((unsigned)n_tile64), dim3(NWD * 64), 0, s, a,
+                         0, (unsigned)n_tile64);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int pairs = sh.B * sh.Hkv, grp = sh.Hq / sh.Hkv;

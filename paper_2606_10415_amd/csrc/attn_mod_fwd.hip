@@ -55,7 +55,6 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
   constexpr int NQG = NW / QSPLIT;                 // query groups of 32
   constexpr int BQW = NQG * 32;                    // queries per workgroup
   constexpr int KBW = KB / QSPLIT;                 // 32-key blocks per slice and wave
-  constexpr bool RAW = !CAP && !BIAS;              // scores stay raw products
   static_assert(QSPLIT == 1 || NQG * DB * 4 * 64 * 16 + NQG * 64 * 8 <= 2 * SM::STAGE, "merge fits in LDS");
   __shared__ __attribute__((aligned(1024))) char smem[2 * SM::STAGE];
   __shared__ int hull_s[2][NW];
@@ -79,10 +78,9 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
 
   const lt_half* Kp = K + (int64_t)b * S * kv_stride + (int64_t)kvh * D;
   const lt_half* Vp = V + (int64_t)b * S * kv_stride + (int64_t)kvh * D;
-  const Cap cap(mod.cap, scale);
-  const float slope2 = BIAS ? mod.slopes[h] * kModLog2e : 0.f;
-  const float c = RAW ? scale * kModLog2e : 1.f;   // stored score -> base-2 units
-  const float cb = scale * kModLog2e;              // raw product -> base-2 units
+  const Score<CAP> sc(mod, scale);
+  const float c = sc.c;
+  const float slope = BIAS ? mod.slopes[h] * kModLog2e / c : 0.f;   // in units of the stored scores
   const float lazy_raw = kLazy / c;
 
   // Q fragments (B operand of S^T = K Q^T): column = this lane's query,
@@ -123,7 +121,7 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
-  float m_run = -INFINITY;   // running max (stored-score units) used as the exponent offset
+  float m_run = -INFINITY;   // running max (stored scores) used as the exponent offset
   float lsum = 0.f;          // this lane's share of the row sum
 
   // K, V rows past S read as zero (no query's interval reaches them)
@@ -150,10 +148,17 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
     if (key0 < wh.hi && key0 + KBW * 32 > wh.lo) {
       // ---- S^T = K Q^T ----
       f32x16 sacc[KBW];
+      const float d0 = (float)(key0 + 4 * g - myq);
+      // keys all up to, or all from, the wave's queries
+      const int side = key0 >= qw0 + 31 ? 1 : key0 + KBW * 32 - 1 <= qw0 ? -1 : 0;
+      if constexpr (BIAS && !CAP) {
+        bias_init(sacc, slope, d0, side);
+      } else {
 #pragma unroll
-      for (int kb = 0; kb < KBW; ++kb)
+        for (int kb = 0; kb < KBW; ++kb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sacc[kb][r] = 0.f;
+          for (int r = 0; r < 16; ++r) sacc[kb][r] = 0.f;
+      }
       // K fragments of step kk+1 are read before the MFMAs of step kk, into
       // the other of two register sets
       auto rdk = [&](int kb, int kk) {
@@ -181,18 +186,15 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
         }
       }
 
-      // ---- cap and bias, to base-2 units ----
-      if constexpr (!RAW) {
-        const float d0 = (float)(key0 + 4 * g - myq);
+      // ---- cap (and bias behind it) ----
+      if constexpr (CAP) {
 #pragma unroll
         for (int kb = 0; kb < KBW; ++kb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            float z = sacc[kb][r];
-            if constexpr (CAP) z = cap.z(cap.u(z));
-            else z *= cb;
-            if constexpr (BIAS) z = fmaf(-slope2, fabsf(d0 + (float)(kb * 32 + 8 * (r >> 2) + (r & 3))), z);
-            sacc[kb][r] = z;
+            sacc[kb][r] = sc.t(sacc[kb][r]);
+            if constexpr (BIAS)
+              sacc[kb][r] = fmaf(-slope, fabsf(d0 + (float)(kb * 32 + 8 * (r >> 2) + (r & 3))), sacc[kb][r]);
           }
       }
 
@@ -235,7 +237,7 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
         float p[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          p[r] = fast_exp2(RAW ? fmaf(sacc[kb][r], c, -mc) : sacc[kb][r] - mc);
+          p[r] = fast_exp2(fmaf(sacc[kb][r], c, -mc));
           lsum += p[r];
         }
 #pragma unroll
@@ -317,7 +319,7 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
       }
     if (g == 0)
       LSE[((int64_t)b * Hq + h) * S + myq] =
-          lo < hi ? m_run * (RAW ? scale : kModLn2) + __logf(lt) : -INFINITY;
+          lo < hi ? (m_run * c + sc.off) * kModLn2 + __logf(lt) : -INFINITY;
   }
 }
 

@@ -61,9 +61,11 @@ inline AttnModPlan attn_mod_plan(int B, int S, int Hq, int Hkv, int causal) {
 }
 // Workspace parts of the backward, in order, each 256-byte aligned: D and the
 // base-2 LSE [B, Hq, S] FP32, the rows' intervals [2][B, S] and the hulls
-// [B][ceil(S / 32)], one chunk's dS blocks, one chunk's partial dK and dV.
+// [B][ceil(S / 32)], a bit for every query of a head (tiles of kSharpTile), one chunk's
+// dS blocks, one chunk's partial dK and dV.
+constexpr int kSharpTile = 128;
 struct AttnModWs {
-  size_t lse2, rows, hulls, ds, part, total;
+  size_t lse2, rows, hulls, sharp, ds, part, total;
 };
 inline AttnModWs attn_mod_ws(int B, int S, int Hq, int Hkv, int D, int causal) {
   const AttnModPlan p = attn_mod_plan(B, S, Hq, Hkv, causal);
@@ -72,7 +74,8 @@ inline AttnModWs attn_mod_ws(int B, int S, int Hq, int Hkv, int D, int causal) {
   w.lse2 = align256((size_t)B * Hq * S * sizeof(float));
   w.rows = 2 * w.lse2;
   w.hulls = w.rows + align256((size_t)2 * B * S * sizeof(int32_t));
-  w.ds = w.hulls + align256((size_t)B * n32 * sizeof(QueryHull));
+  w.sharp = w.hulls + align256((size_t)B * n32 * sizeof(QueryHull));
+  w.ds = w.sharp + align256((size_t)B * Hq * (((size_t)S + kSharpTile - 1) / kSharpTile) * (kSharpTile / 8));
   w.part = w.ds + align256((size_t)p.chunk * (Hq / Hkv) * (size_t)attn_bwd_ds_blocks(S, causal) * kDsBlockBytes);
   w.total = w.part + (p.nsplit > 1 ? align256((size_t)2 * p.chunk * p.nsplit * S * D * sizeof(float)) : 0);
   return w;
@@ -98,6 +101,7 @@ struct AttnModBwdArgs {
   float* lse2;
   int32_t* rows;
   QueryHull* hulls;
+  uint32_t* sharp;
   lt_half* ds;
   float* part;
 };
