@@ -453,6 +453,8 @@ lt_status lt_rope_f16(lt_half* X, int64_t row_stride, int B, int S, int heads,
  *   prefix mask: causal = 0, HI = max(i + 1, end of the prefix).  A sliding window:
  *   LO = i - width + 1, causal = 1.  A padded batch: HI = the row's length, and
  *   HI = 0 for the padding.  A query that sees no key gets O = 0 and LSE = -inf.
+ *   Non-finite values reach only those that see them: keys that no query sees and
+ *   queries that see nothing may hold anything (slower where they do).
  *   slopes: [Hq] FP32 device array or NULL.  cap: 0 for none, else up to 1000.
  *   Layouts, head grouping and errors as lt_attn_fwd, and
  *   LT_ERR_INVALID_ARG for a cap that is negative or not finite;

@@ -71,6 +71,48 @@ __device__ __forceinline__ void bias_init(f32x16 (&acc)[N], float slope, float d
   }
 }
 
+// Non-finite values in places that a query does not see.  The products run over whole
+// tiles, and 0 x NaN is NaN: a probability or dS of zero does not keep out a
+// non-finite V, K, Q or dO.  The kernels pay nothing for that case on the way: where an
+// accumulator of a wave ends up non-finite, they form it again one (query, key) pair at a time,
+// over the pairs that see each other.
+template <int DB>
+__device__ __forceinline__ bool all_finite(const f32x16 (&acc)[DB]) {
+  float m = 0.f;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) m = fmaf(acc[db][r], 0.f, m);     // 0, or NaN
+  return __builtin_amdgcn_ballot_w64(!(m == 0.f)) == 0;
+}
+// this lane's half of a row product: features kk * 16 + 8 g + 0..7 of both
+template <int KK>
+__device__ __forceinline__ float half_dot(const half8 (&f)[KK], const lt_half* row) {
+  float s = 0.f;
+#pragma nounroll
+  for (int kk = 0; kk < KK; ++kk) {
+    half8 x = f[0];
+#pragma unroll
+    for (int i = 1; i < KK; ++i) x = kk == i ? f[i] : x;           // constant register indices
+    const half8 y = as_half8(ld16(row + kk * 16));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf((float)x[e], (float)y[e], s);
+  }
+  return s;
+}
+// acc[db][4 rq + e] += w * row[db * 32 + 8 rq + 4 g + e] where `on`
+template <int DB>
+__device__ __forceinline__ void add_row(f32x16 (&acc)[DB], bool on, float w, const lt_half* row, int g) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int rq = 0; rq < 4; ++rq) {
+      const half4 x = *reinterpret_cast<const half4*>(row + db * 32 + 8 * rq + 4 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[db][4 * rq + e] = on ? fmaf(w, (float)x[e], acc[db][4 * rq + e]) : acc[db][4 * rq + e];
+    }
+}
+
 __device__ __forceinline__ int wave_min32(int v) {   // over lane % 32
 #pragma unroll
   for (int m = 16; m >= 1; m >>= 1) v = min(v, __shfl_xor(v, m));

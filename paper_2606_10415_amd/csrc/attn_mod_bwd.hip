@@ -715,6 +715,43 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
       }
   }
 
+  if (!(all_finite(dkacc) & all_finite(dvacc))) {  // a non-finite Q or dO somewhere in the tiles
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        dkacc[db][r] = 0.f;
+        dvacc[db][r] = 0.f;
+      }
+    const int64_t krow = mykey < S ? mykey : S - 1;
+    half8 vf[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) vf[kk] = as_half8(ld16(Vp + krow * a.kv_stride + kk * 16 + g * 8));
+#pragma nounroll
+    for (int it = 0; it < n_iter; ++it) {
+      int jh, qb;
+      pair_of(it, jh, qb);
+      const int h = kvh * G + jh;
+      const float slope = BIAS ? a.mod.slopes[h] * kModLog2e / sc.c : 0.f;
+#pragma nounroll
+      for (int q = qb; q < min(qb + BQA, S); ++q) {
+        const int64_t row = (int64_t)b * S + q, ri = ((int64_t)b * Hq + h) * S + q;
+        const lt_half* qp = a.Q + row * a.q_stride + (int64_t)h * D;
+        const lt_half* gp = a.dO + row * a.o_stride + (int64_t)h * D;
+        float s = half_dot(kf, qp + 8 * g), dp = half_dot(vf, gp + 8 * g);
+        s += __shfl_xor(s, 32);
+        dp += __shfl_xor(dp, 32);
+        float t = sc.t(s), w = dp - a.delta[ri];
+        if constexpr (CAP) w *= -4.f * t * (1.f + t);
+        if constexpr (BIAS) t = fmaf(-slope, fabsf((float)(q - mykey)), t);
+        const float p = fast_exp2(fmaf(t, sc.c, -a.lse2[ri]));
+        const bool see = (mykey >= a.rows[(int64_t)b * S + q]) & (mykey < a.rows[(int64_t)(B + b) * S + q]);
+        add_row(dvacc, see, p, gp, g);
+        add_row(dkacc, see, p * w, qp, g);
+      }
+    }
+  }
+
   // ---- write dK = scale * acc, dV (or this share's FP32 partial sums) ----
   if (mykey >= S) return;
   if (nsh > 1) {
@@ -932,6 +969,20 @@ attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
     const int pos = lane & 31;
     const int q = qg * 32 + 8 * ((pos & 15) >> 2) + 4 * (pos >> 4) + (pos & 3);
     const int g = lane >> 5;
+    if (!all_finite(acc)) {                        // a non-finite K somewhere in the tiles
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
+      int lo, hi;
+      row_interval(a.mod, causal, b, S, q, lo, hi);
+#pragma nounroll
+      for (int k = kg0 * 32; k < min(kg_end * 32, S); ++k) {
+        const char* el = dsq + (int64_t)(k >> 5) * kDsBlockBytes + ((k & 31) + 32 * (pos >> 4)) * 32 + (pos & 15) * 2;
+        add_row(acc, (k >= lo) & (k < hi), (float)*reinterpret_cast<const _Float16*>(el),
+                Kp + (int64_t)k * a.kv_stride, g);
+      }
+    }
     if (q < S) {
       lt_half* qp = a.dQ + ((int64_t)b * S + q) * a.dq_stride + (int64_t)h * D;
 #pragma unroll

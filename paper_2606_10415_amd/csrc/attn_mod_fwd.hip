@@ -305,6 +305,21 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
 
   // ---- normalise and store O, LSE ----
   const float lt = lsum + __shfl_xor(lsum, 32);
+  if (!all_finite(oacc)) {                         // a non-finite V somewhere in the tiles
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
+    const float mc = m_run == -INFINITY ? 0.f : m_run * c;
+#pragma nounroll
+    for (int j = wh.lo; j < wh.hi; ++j) {
+      float s = half_dot(qf, Kp + (int64_t)j * kv_stride + 8 * g);
+      s += __shfl_xor(s, 32);
+      float t = sc.t(s);
+      if constexpr (BIAS) t = fmaf(-slope, fabsf((float)(j - myq)), t);
+      add_row(oacc, (j >= lo) & (j < hi), fast_exp2(fmaf(t, c, -mc)), Vp + (int64_t)j * kv_stride, g);
+    }
+  }
   if (myq < S) {
     const float inv = lo < hi ? 1.f / lt : 0.f;
     lt_half* op = O + ((int64_t)b * S + myq) * o_stride + (int64_t)h * D;

@@ -306,3 +306,87 @@ def test_results_repeat_bitwise(env):
     b = run_gpu(env, x, 2, 128, 0.09, mask, 30.0, slopes_of(8))
     for n in a:
         assert np.array_equal(a[n].view(np.uint8), b[n].view(np.uint8)), n
+
+
+BAD = [float("nan"), float("inf"), -float("inf")]
+
+
+@pytest.mark.parametrize("B,S,Hq,Hkv,D,cap,biased", [(2, 200, 2, 1, 64, 0.0, False), (1, 700, 4, 4, 128, 20.0, True),
+                                                    (1, 333, 16, 2, 128, 0.0, True), (6, 450, 64, 64, 64, 0.0, False)])
+@pytest.mark.parametrize("bad", BAD, ids=str)
+def test_non_finite_padding_takes_no_part(env, B, S, Hq, Hkv, D, cap, biased, bad):
+    """What no query sees, and queries that see nothing, may hold anything."""
+    print("non-finite padding", B, S, Hq, Hkv, D, cap, biased, bad, flush=True)
+    rng, x = inputs(50 + S, B, S, Hq, Hkv, D)
+    mask = make_mask("pad", B, S, rng)
+    n = mask[1].max(1)
+    for b in range(B):
+        for name in ("Q", "K", "V", "dO"):
+            x[name][b, n[b]:] = bad
+    slopes = slopes_of(Hq) if biased else None
+    got = run_gpu(env, x, Hkv, D, 0.1, mask, cap, slopes)
+    check(got, x, Hkv, 0.1, mask, cap, slopes, None if B < 4 else {(0, 0), (1, 1), (B - 1, Hkv - 1)})
+    for b in range(B):
+        assert np.all(got["dK"][b, n[b]:] == 0) and np.all(got["dV"][b, n[b]:] == 0)
+
+
+@pytest.mark.parametrize("B,S,Hq,Hkv,D,cap,biased,first,last", [
+    (1, 300, 2, 2, 64, 0.0, False, 100, 140), (2, 600, 8, 2, 128, 30.0, False, 257, 259),
+    (1, 1100, 16, 16, 128, 0.0, True, 40, 700), (3, 130, 3, 1, 64, 15.0, True, 0, 64)])
+def test_non_finite_document_stays_to_itself(env, B, S, Hq, Hkv, D, cap, biased, first, last):
+    """One document of NaN and infinities: the others have the results of their own values."""
+    print("non-finite document", B, S, Hq, Hkv, D, cap, biased, first, last, flush=True)
+    rng, x = inputs(60 + S, B, S, Hq, Hkv, D)
+    lo = np.zeros((B, S), np.int32)
+    lo[:, first:] = first
+    lo[:, last:] = last
+    mask, slopes = (lo, None, 1), slopes_of(Hq) if biased else None
+    clean = {k: v.copy() for k, v in x.items()}
+    for k in clean:
+        clean[k][:, first:last] = 0
+    want = run_gpu(env, clean, Hkv, D, 0.1, mask, cap, slopes)
+    for name in ("Q", "K", "V", "dO"):
+        x[name][:, first:last] = rng.choice(np.array(BAD + [1.0], np.float16), size=x[name][:, first:last].shape)
+    x["Q"][:, first:last, :, 0] = np.nan
+    got = run_gpu(env, x, Hkv, D, 0.1, mask, cap, slopes)
+    assert np.isnan(got["O"][:, first:last].astype(np.float32)).all(-1).all()
+    for name in got:                                 # judge the other documents
+        if name == "LSE":
+            got[name][:, :, first:last] = want[name][:, :, first:last]
+        else:
+            got[name][:, first:last] = want[name][:, first:last]
+    check(got, clean, Hkv, 0.1, mask, cap, slopes)
+
+
+def test_non_finite_value_reaches_those_who_see_it(env):
+    """An infinite V element under a causal mask: that feature of the queries from there on, nothing else."""
+    B, S, H_, D = 1, 150, 2, 64
+    rng, x = inputs(71, B, S, H_, H_, D)
+    x["V"][0, 70, 1, 5] = np.inf
+    clean = dict(x, V=x["V"].copy())
+    clean["V"][0, 70, 1, 5] = 0
+    mask = (None, None, 1)
+    got = run_gpu(env, x, H_, D, 0.1, mask, 0.0, None, bwd=False)
+    want = run_gpu(env, clean, H_, D, 0.1, mask, 0.0, None, bwd=False)
+    o = got["O"]
+    assert np.all(np.isposinf(o[0, 70:, 1, 5]))
+    o[0, 70:, 1, 5] = want["O"][0, 70:, 1, 5]
+    check(got, clean, H_, 0.1, mask, 0.0, None)
+
+
+@pytest.mark.parametrize("kind,cap,std", [("window", 50.0, 3.0), ("causal", 0.0, 3.0)])
+def test_gradients_of_concentrated_softmax(env, kind, cap, std):
+    """Scores of deviation 9, so that rows rest on a few keys and dP - D cancels.  dQ and dK carry two
+    independent FP16 roundings (dS, the output), each at most 2^-11 / sqrt(3) of the value in the mean square:
+    sqrt(2 / 3) 2^-11 = 4.0e-4 of the norm."""
+    B, S, Hq, Hkv, D = 1, 768, 2, 2, 128
+    rng, x = inputs(81, B, S, Hq, Hkv, D, std)
+    mask, scale = make_mask(kind, B, S, rng), 1 / math.sqrt(D)
+    got = run_gpu(env, x, Hkv, D, scale, mask, cap, None)
+    l, h_ = oracle.intervals(S, None if mask[0] is None else mask[0][0], None, True)
+    for h in range(Hq):
+        r = oracle.attn_mod_head(*(x[n][0, :, h] for n in "QKV"), scale, l, h_, cap, 0.0, x["dO"][0, :, h])
+        for n, m in (("dQ", "dq"), ("dK", "dk")):
+            e = np.linalg.norm(got[n][0, :, h].astype(np.float64) - r[m]) / np.linalg.norm(r[m])
+            print(kind, h, n, e, flush=True)
+            assert e <= math.sqrt(2 / 3) * H
