@@ -477,7 +477,7 @@ lt_status lt_attn_mod_fwd(const lt_half* Q, const lt_half* K, const lt_half* V,
  *   query that sees no key gets dQ = 0, a key that no query sees dK = dV = 0.
  *   LO, HI, slopes, cap, scale and causal as given to the forward, O and LSE as
  *   it wrote them.  dS is kept in FP16 between the passes, as in lt_attn_bwd,
- *   for part of the (batch, key/value head) pairs at a time (about 4 GiB, or
+ *   for part of the (batch, key/value head) pairs at a time (about 8 GiB, or
  *   one pair's if that is more).  Errors as the forward and lt_attn_bwd; the
  *   workspace (256-byte aligned) needs lt_attn_mod_bwd_workspace_size bytes, 0
  *   for invalid sizes.

@@ -39,25 +39,55 @@ struct QueryHull {
 // at a time, each chunk's dK/dV pass followed by its dQ pass, so that the dS
 // blocks in the workspace are one chunk's: a chunk is as large as keeps them
 // within kModDsBudget, but has at least the workgroups to fill the CUs twice.
-// ktile and nsplit as in DkdvPlan, for one chunk; the shares of a key tile are
-// equal parts of its (query head, visible 64-query block) pairs.
-constexpr int64_t kModDsBudget = (int64_t)4 << 30;
+// (Chunks small enough for the 256 MB last-level cache lose: 4096 tokens of 40 heads
+// in 4 chunks 1240 us, in one 990.)
+//   ktile: keys per dK/dV workgroup, 256 or 128; nsplit: equal shares of a key tile's
+// (query head, visible 64-query block) pairs, with partial sums when above 1.  Both
+// by the estimated time of the pass: a 64-query block of a 256-key tile takes 4.3 us
+// at D = 128 (0.55 of it for 128 keys, 1.8 at least), a workgroup's start and end 6, the
+// sum pass 4 and what its partials take at 5 TB/s.  The interval of each query is on
+// the device only, so that a causal mask is taken for the mean of equal key tiles
+// (documents, windows) and of shrinking ones.  Measured against shares by the rule of
+// lt_attn_bwd over 13 shapes x 4 masks: 0.96 of the time in the mean, 4 padded sequences of
+// 333 tokens of 16 heads 34 us against 49, 2048 tokens of 40:8 heads 210 against 234.
+constexpr int64_t kModDsBudget = (int64_t)8 << 30;
 constexpr int kModMaxS = 1 << 19;         // the dK/dV pass lists a tile's 64-query blocks in LDS
+constexpr int kModMaxShares = 16;
 struct AttnModPlan {
   int chunk, ktile, nsplit;
 };
-inline AttnModPlan attn_mod_plan(int B, int S, int Hq, int Hkv, int causal) {
-  const int64_t pairs = (int64_t)B * Hkv, grp = Hq / Hkv;
+inline AttnModPlan attn_mod_plan(int B, int S, int Hq, int Hkv, int D, int causal) {
+  constexpr int64_t kCUs = 256;
+  const int64_t pairs = (int64_t)B * Hkv, grp = Hq / Hkv, n_qb = ((int64_t)S + 63) / 64;
   const int64_t per_pair = grp * attn_bwd_ds_blocks(S, causal) * kDsBlockBytes;
-  const int64_t n_kt = ((int64_t)S + 255) / 256;
-  int64_t fill = 512 / (n_kt * grp);
-  int64_t fit = kModDsBudget / per_pair;
+  const int64_t fill = 2 * kCUs / ((((int64_t)S + 255) / 256) * grp);
+  const int64_t fit = kModDsBudget / per_pair;
   int64_t c = fit > fill ? fit : fill;
   c = c < 1 ? 1 : c > pairs ? pairs : c;
   const int64_t chunks = (pairs + c - 1) / c;
   c = (pairs + chunks - 1) / chunks;
-  const DkdvPlan p = attn_bwd_dkdv_plan(1, S, (int)(c * grp), (int)c);
-  return {(int)c, p.ktile, p.nsplit};
+  AttnModPlan best = {(int)c, 256, 1};
+  double best_us = 0;
+  for (int ktile = 256; ktile >= 128; ktile /= 2) {
+    const int64_t n_kt = ((int64_t)S + ktile - 1) / ktile;
+    double block = 4.3 * D / 128 * (ktile == 256 ? 1.0 : 0.55);
+    if (block < 1.8) block = 1.8;
+    for (int n = 1; n <= kModMaxShares && (n == 1 || n <= grp * (n_qb < 4 ? n_qb : 4)); ++n) {
+      const int64_t longest = (grp * n_qb + n - 1) / n, wgs = n_kt * c * n;
+      double blocks = (double)((wgs + kCUs - 1) / kCUs * longest);
+      if (causal) {
+        const double even = 0.54 * (double)(grp * n_qb * n_kt * c) / kCUs;
+        blocks = 0.5 * blocks + 0.5 * (even > (double)longest ? even : (double)longest);
+      }
+      double us = blocks * block + 6.0 * (wgs > kCUs ? (double)wgs / kCUs : 1.0);
+      if (n > 1) us += 4.0 + n + (double)(n * c) * S * D * 16 / 5.0e6;
+      if (best_us == 0 || us < best_us) {
+        best_us = us;
+        best = {(int)c, ktile, n};
+      }
+    }
+  }
+  return best;
 }
 // Workspace parts of the backward, in order, each 256-byte aligned: D and the
 // base-2 LSE [B, Hq, S] FP32, the rows' intervals [2][B, S] and the hulls
@@ -68,7 +98,7 @@ struct AttnModWs {
   size_t lse2, rows, hulls, sharp, ds, part, total;
 };
 inline AttnModWs attn_mod_ws(int B, int S, int Hq, int Hkv, int D, int causal) {
-  const AttnModPlan p = attn_mod_plan(B, S, Hq, Hkv, causal);
+  const AttnModPlan p = attn_mod_plan(B, S, Hq, Hkv, D, causal);
   const size_t n32 = ((size_t)S + 31) / 32;
   AttnModWs w;
   w.lse2 = align256((size_t)B * Hq * S * sizeof(float));

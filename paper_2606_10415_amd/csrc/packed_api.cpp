@@ -168,7 +168,7 @@ lt_status lt_attn_mod_bwd(const lt_half* Q, const lt_half* K, const lt_half* V, 
                        dV,
                        dq_row_stride,
                        dkv_row_stride,
-                       lt::attn_mod_plan(B, S, Hq, Hkv, causal),
+                       lt::attn_mod_plan(B, S, Hq, Hkv, D, causal),
                        reinterpret_cast<float*>(ws),
                        reinterpret_cast<float*>(ws + w.lse2),
                        reinterpret_cast<int32_t*>(ws + w.rows),

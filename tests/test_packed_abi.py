@@ -137,11 +137,12 @@ def test_workspace_sizes():
         return (2 * up(4 * B * Hq * S) + up(8 * B * S) + up(16 * B * n32) + up(16 * B * Hq * -(-S // 128)) +
                 up(chunk * (Hq // Hkv) * blocks * 2048) +
                 (up(8 * chunk * nsplit * S * D) if nsplit > 1 else 0))
-    # enough key tiles: one chunk, no shares; a short sequence of few heads: shares
+    # enough key tiles: one chunk, no shares; short sequences of few heads: shares, or not
     assert lt.lt_attn_mod_bwd_workspace_size(1, 4096, 32, 32, 128, 1) == attn(1, 4096, 32, 32, 128, 1, 32, 1)
-    assert lt.lt_attn_mod_bwd_workspace_size(2, 100, 8, 2, 128, 0) == attn(2, 100, 8, 2, 128, 0, 4, 8)
-    # 4.3 GB of dS blocks: two chunks of four pairs
-    assert lt.lt_attn_mod_bwd_workspace_size(1, 8192, 64, 8, 128, 1) == attn(1, 8192, 64, 8, 128, 1, 4, 4)
+    assert lt.lt_attn_mod_bwd_workspace_size(1, 2048, 40, 8, 128, 1) == attn(1, 2048, 40, 8, 128, 1, 8, 4)
+    assert lt.lt_attn_mod_bwd_workspace_size(4, 333, 16, 16, 64, 0) == attn(4, 333, 16, 16, 64, 0, 64, 1)
+    # 8.6 GB of dS blocks: two chunks of eight pairs
+    assert lt.lt_attn_mod_bwd_workspace_size(2, 8192, 64, 8, 128, 1) == attn(2, 8192, 64, 8, 128, 1, 8, 2)
     # 128k tokens: a pair at a time, whatever it takes
     assert lt.lt_attn_mod_bwd_workspace_size(1, 131072, 8, 8, 128, 1) == attn(1, 131072, 8, 8, 128, 1, 1, 1)
     for bad in ((0, 16, 2, 1, 64, 1), (1, 16, 3, 2, 64, 1), (1, 16, 2, 1, 96, 1), (1, 16, 2, 1, 64, 2),
