@@ -170,7 +170,7 @@ attn_mod_delta_kernel(const AttnModBwdArgs a, int all, unsigned n_tile) {
   const int B = a.sh.B, S = a.sh.S, Hq = a.sh.Hq, Hkv = a.sh.Hkv, causal = a.sh.causal;
   if (blockIdx.x >= n_tile) return rows_and_hulls(a, blockIdx.x - n_tile);
   const int n_qt = (S + BQW - 1) / BQW;
-  const int qt = causal ? n_qt - 1 - (int)(blockIdx.x / (B * Hq)) : (int)(blockIdx.x / (B * Hq));
+  const int qt = n_qt - 1 - (int)(blockIdx.x / (B * Hq));   // later queries mostly see more keys: longest first
   int b, h;
   query_head(blockIdx.x % (B * Hq), B, Hq, Hkv, b, h);
   const uint32_t* marks = a.sharp + ((int64_t)b * Hq + h) * ((S + kTile - 1) / kTile) * (kTile / 32) + qt * NQG;
@@ -872,7 +872,7 @@ attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
   const int n_qt = (S + BQQ - 1) / BQQ;
   const int G = Hq / Hkv;
   const int slot = blockIdx.x / (nb * G);
-  const int qt = causal ? n_qt - 1 - slot : slot;
+  const int qt = n_qt - 1 - slot;                  // later queries mostly see more keys: longest first
   // the query heads of one kv head on one XCD where the chunk is a multiple of 8
   const int lbkv = (blockIdx.x % (nb * G)) % nb;
   const int j = (blockIdx.x % (nb * G)) / nb;

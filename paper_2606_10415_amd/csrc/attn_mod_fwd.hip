@@ -68,7 +68,7 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
   const int kpart = wave / NQG;                    // which block of each slice (QSPLIT = 2)
 
   const int n_qt = (S + BQW - 1) / BQW;
-  const int qt = causal ? n_qt - 1 - (int)(blockIdx.x / (B * Hq)) : (int)(blockIdx.x / (B * Hq));
+  const int qt = n_qt - 1 - (int)(blockIdx.x / (B * Hq));   // later queries mostly see more keys: longest first
   int b, h;
   query_head(blockIdx.x % (B * Hq), B, Hq, Hkv, b, h);
   const int kvh = h / (Hq / Hkv);

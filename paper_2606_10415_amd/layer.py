@@ -20,6 +20,12 @@ and RMSNorm backward (with the residual gradient added in the same pass):
 A norm with a QKV bias (Qwen2.5) adds it in the QKV GEMM's epilogue and
 takes its gradient as the column sum of dQKV after the inverse rotation.
 
+A norm with weights for the query and key heads (``wq``, ``wk``) normalises each
+head and rotates it in one pass, out of QKV into QKr (the backward needs both);
+without a rotary base nothing is rotated.  ``attention`` (packing.Attention)
+replaces the causal attention by the one with its intervals of visible keys,
+score cap and distance bias, and gives the positions of a packed batch.
+
 With ``fuse_swiglu`` the SwiGLU gate runs in the epilogues of the gate/up
 GEMM (A from the FP32 accumulators, GU still stored for the backward) and of
 the down-projection dgrad (dGU written directly, dA never stored).
@@ -37,13 +43,14 @@ class DecoderLayer:
 
     ``shape`` needs attributes B, S, H, Hq, Hkv, D, F.  ``params`` maps
     X, dY, Wqkv, Wo, Wgu, Wd to float16 tensors (host or device).  ``norm``
-    (optional) has attributes wn1, wn2 (RMSNorm weights [H]), eps, rope_base and
-    optionally bqkv (QKV projection bias, or None).
+    (optional) has attributes wn1, wn2 (RMSNorm weights [H]), eps, rope_base (or
+    None) and optionally bqkv (QKV projection bias), wq and wk (head norm weights
+    [D]), each may be None.  ``attention`` (optional) is a packing.Attention.
     ``fuse_swiglu`` selects the GEMMs with the SwiGLU epilogues.
     """
 
     def __init__(self, shape, params, device="cuda", norm=None, fuse_swiglu=True,
-                 share_bwd=None, share_acts=None):
+                 share_bwd=None, share_acts=None, attention=None):
         self.sh = sh = shape
         self.fuse_swiglu = bool(fuse_swiglu)
         self.accumulate = False
@@ -65,14 +72,38 @@ class DecoderLayer:
         self.Wgu = dev(params["Wgu"])
         self.Wd = dev(params["Wd"])
 
+        self.rope = norm is not None and norm.rope_base is not None
+        self.qk_norm = norm is not None and getattr(norm, "wq", None) is not None
+        if self.qk_norm and not self.rope:
+            raise ValueError("QK norm comes with the rotary embedding: rope_base must be given")
+        self.attn = attention
+        pos = None
+        if attention is not None:
+            def rows(x, name):
+                if x is None:
+                    return None
+                t = torch.as_tensor(x).to(self.dev, torch.int32).contiguous()
+                if tuple(t.shape) != (sh.B, sh.S):
+                    raise ValueError(f"attention.{name} must be [{sh.B}, {sh.S}], got {tuple(t.shape)}")
+                return t
+            self.LO, self.HI = rows(attention.lo, "lo"), rows(attention.hi, "hi")
+            self.slopes = None
+            if attention.slopes is not None:
+                self.slopes = torch.as_tensor(attention.slopes).to(self.dev, torch.float32).contiguous()
+                if tuple(self.slopes.shape) != (sh.Hq,):
+                    raise ValueError(f"attention.slopes must have {sh.Hq} entries")
+            pos = rows(attention.pos, "pos") if self.qk_norm else None
+
         e = lambda *s: torch.empty(*s, dtype=torch.float16, device=self.dev)
         # forward activations the backward reads (shareable between layers
         # whose forward is recomputed right before their backward)
         if share_acts is not None:
-            for k in ("QKV", "O", "LSE", "H1", "GU", "A"):
+            for k in ("QKV", "QKr", "O", "LSE", "H1", "GU", "A"):
                 setattr(self, k, getattr(share_acts, k))
         else:
             self.QKV = e(T, self.qkv)
+            # rotated Q and K, rows as far apart as QKV's (attention takes K and V with one row stride)
+            self.QKr = e(T, self.qkv) if self.qk_norm else self.QKV
             self.O = e(T, self.hd)
             self.LSE = torch.empty(sh.B, sh.Hq, sh.S, dtype=torch.float32, device=self.dev)
             self.H1 = e(T, sh.H)
@@ -91,7 +122,10 @@ class DecoderLayer:
             self.dO = e(T, self.hd)
             self.dQKV = e(T, self.qkv)
             self.dX = e(T, sh.H)
-            self.ws_bytes = lt.lt_attn_bwd_workspace_size(sh.B, sh.S, sh.Hq, sh.Hkv, sh.D, 1)
+            if attention is not None:
+                self.ws_bytes = lt.lt_attn_mod_bwd_workspace_size(sh.B, sh.S, sh.Hq, sh.Hkv, sh.D, attention.causal)
+            else:
+                self.ws_bytes = lt.lt_attn_bwd_workspace_size(sh.B, sh.S, sh.Hq, sh.Hkv, sh.D, 1)
             self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.dev)
             # split-K workspace of the plain GEMM calls (one at a time on the
             # stream); the fused SwiGLU GEMMs take none
@@ -119,8 +153,17 @@ class DecoderLayer:
             f32 = lambda *s_: torch.empty(*s_, dtype=torch.float32, device=self.dev)
             self.rstd1 = f32(T)
             self.rstd2 = f32(T)
-            self.CS = f32(sh.S, sh.D // 2, 2)
-            lt.lt_rope_table(self.CS, sh.S, sh.D, float(norm.rope_base))
+            if self.rope:
+                self.P = max(sh.S, int(pos.max()) + 1) if pos is not None else sh.S
+                self.CS = f32(self.P, sh.D // 2, 2)
+                lt.lt_rope_table(self.CS, self.P, sh.D, float(norm.rope_base))
+            if self.qk_norm:
+                self.pos = pos
+                self.Wq, self.Wk = dev(norm.wq), dev(norm.wk)
+                self.dWq, self.dWk = e(sh.D), e(sh.D)
+                self.rstd_qk = f32(T, sh.Hq + sh.Hkv)
+                self.qkn_ws_bytes = lt.lt_qknorm_rope_bwd_workspace_size(sh.B, sh.S, sh.Hq, sh.Hkv, sh.D)
+                self.qkn_ws = torch.empty(self.qkn_ws_bytes, dtype=torch.uint8, device=self.dev)
             self.rms_ws_bytes = lt.lt_rmsnorm_bwd_workspace_size(T, sh.H)
             self.rms_ws = torch.empty(self.rms_ws_bytes, dtype=torch.uint8, device=self.dev)
         self.bqkv = None
@@ -145,6 +188,11 @@ class DecoderLayer:
         p = base.data_ptr()
         return p, p + 2 * self.hd, p + 2 * (self.hd + self.sh.Hkv * self.sh.D)
 
+    def _qkv_ptrs(self):
+        """Q and K as attention reads them (rotated), and V."""
+        q, k, _ = self._attn_ptrs(self.QKr)
+        return q, k, self._attn_ptrs(self.QKV)[2]
+
     def forward(self, stream=None, hook=None):
         """Layer forward.  ``hook(name)`` (optional) is called after each launch."""
         sh, T = self.sh, self.T
@@ -162,12 +210,20 @@ class DecoderLayer:
             self._gemm(0, 1, T, self.qkv, sh.H, xin, sh.H, self.Wqkv, sh.H, 0.0, self.QKV, self.qkv,
                        stream)
         mark("qkv_fwd")
-        if self.norm is not None:
+        if self.qk_norm:
+            lt.lt_qknorm_rope_fwd(self.QKV, self.qkv, self.Wq, self.Wk, self.CS, self.P, self.pos, self.QKr, self.qkv,
+                                  self.rstd_qk, sh.B, sh.S, sh.Hq, sh.Hkv, sh.D, self.eps, stream)
+            mark("qknorm_fwd")
+        elif self.rope:
             lt.lt_rope_f16(self.QKV, self.qkv, sh.B, sh.S, sh.Hq + sh.Hkv, sh.D, self.CS, 0, stream)
             mark("rope_fwd")
-        q, k, v = self._attn_ptrs(self.QKV)
-        lt.lt_attn_fwd(q, k, v, self.qkv, self.qkv, self.O, self.hd, self.LSE, sh.B, sh.S, sh.Hq,
-                       sh.Hkv, sh.D, self.scale, 1, stream)
+        q, k, v = self._qkv_ptrs()
+        if self.attn is not None:
+            lt.lt_attn_mod_fwd(q, k, v, self.qkv, self.qkv, self.O, self.hd, self.LSE, self.LO, self.HI, self.slopes,
+                               self.attn.cap, sh.B, sh.S, sh.Hq, sh.Hkv, sh.D, self.scale, self.attn.causal, stream)
+        else:
+            lt.lt_attn_fwd(q, k, v, self.qkv, self.qkv, self.O, self.hd, self.LSE, sh.B, sh.S, sh.Hq,
+                           sh.Hkv, sh.D, self.scale, 1, stream)
         mark("attn_fwd")
         self._gemm(0, 1, T, sh.H, self.hd, self.O, self.hd, self.Wo, self.hd, 1.0, self.H1, sh.H,
                    stream, R=self.X, ldr=sh.H)
@@ -236,13 +292,23 @@ class DecoderLayer:
                    stream)
         mark("o_dgrad")
         # attention
-        q, k, v = self._attn_ptrs(self.QKV)
+        q, k, v = self._qkv_ptrs()
         dq, dk, dv = self._attn_ptrs(self.dQKV)
-        lt.lt_attn_bwd(q, k, v, self.qkv, self.qkv, self.O, self.dO, self.hd, self.LSE, dq, dk, dv,
-                       self.qkv, self.qkv, self.ws, self.ws_bytes, sh.B, sh.S, sh.Hq, sh.Hkv, sh.D,
-                       self.scale, 1, stream)
+        if self.attn is not None:
+            lt.lt_attn_mod_bwd(q, k, v, self.qkv, self.qkv, self.O, self.dO, self.hd, self.LSE, self.LO, self.HI,
+                               self.slopes, self.attn.cap, dq, dk, dv, self.qkv, self.qkv, self.ws, self.ws_bytes,
+                               sh.B, sh.S, sh.Hq, sh.Hkv, sh.D, self.scale, self.attn.causal, stream)
+        else:
+            lt.lt_attn_bwd(q, k, v, self.qkv, self.qkv, self.O, self.dO, self.hd, self.LSE, dq, dk, dv,
+                           self.qkv, self.qkv, self.ws, self.ws_bytes, sh.B, sh.S, sh.Hq, sh.Hkv, sh.D,
+                           self.scale, 1, stream)
         mark("attn_bwd")
-        if self.norm is not None:
+        if self.qk_norm:
+            lt.lt_qknorm_rope_bwd(self.dQKV, self.qkv, self.QKV, self.qkv, self.Wq, self.Wk, self.rstd_qk, self.CS,
+                                  self.P, self.pos, self.dQKV, self.qkv, self.dWq, self.dWk, self.qkn_ws,
+                                  self.qkn_ws_bytes, sh.B, sh.S, sh.Hq, sh.Hkv, sh.D, stream)
+            mark("qknorm_bwd")
+        elif self.rope:
             lt.lt_rope_f16(self.dQKV, self.qkv, sh.B, sh.S, sh.Hq + sh.Hkv, sh.D, self.CS, 1, stream)
             mark("rope_bwd")
         if self.bqkv is not None:

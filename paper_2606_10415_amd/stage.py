@@ -16,6 +16,11 @@ Activation policies (Sec. 4.3):
 Layers with RMSNorm / rotary embedding / QKV bias (``norm``) run single
 micro-batches only (their norm and bias gradients are not accumulated).
 
+With a token embedding (``embed``, the first stage of a pipeline) the
+micro-batches are token ids: the embedding's rows are the layers' input, and the
+gradient of the table accumulates over the micro-batches like the other weight
+gradients.  ``attention`` (packing.Attention) goes to every layer.
+
 Backward temporaries (dA, dGU, dH1, dO, dQKV and the attention workspace) are
 shared by all layers; the input gradients alternate between two buffers.  With
 ``optimizer_state`` the stage also holds the FP32 master weights and two Adam
@@ -25,12 +30,15 @@ the measured peak memory covers the planner's state term.
 
 import torch
 
+from . import lt
 from .layer import DecoderLayer
 
 
 class Stage:
     def __init__(self, shape, layers, act="full", seed=0, device="cuda", optimizer_state=False,
-                 weights=None, norm=None):
+                 weights=None, norm=None, attention=None, embed=None, embed_scale=1.0):
+        """``embed``: FP16 table [V, H] (host or device) or its number of rows V, drawn
+        N(0, 0.02^2); the layers' input is ``embed_scale`` times its rows."""
         if act not in ("full", "ckpt"):
             raise ValueError("act must be 'full' or 'ckpt'")
         self.sh = sh = shape
@@ -57,17 +65,35 @@ class Stage:
             first = self.layers[0] if self.layers else None
             share_acts = first if (act == "ckpt" and first is not None) else None
             self.layers.append(DecoderLayer(sh, p, device=device, norm=norm, share_bwd=first,
-                                            share_acts=share_acts))
+                                            share_acts=share_acts, attention=attention))
         # input gradients alternate between two buffers (a layer reads the one
         # written by the layer above and writes the other)
         self.dx = [self.layers[0].dX, torch.empty(T, sh.H, dtype=torch.float16, device=self.dev)]
+        self.We = None
+        if embed is not None:
+            if isinstance(embed, int):
+                embed = rnd(embed, sh.H, std=0.02)
+            t = embed if isinstance(embed, torch.Tensor) else torch.from_numpy(embed)
+            self.We = t.to(self.dev, torch.float16).contiguous()
+            if self.We.dim() != 2 or self.We.shape[1] != sh.H:
+                raise ValueError(f"embed must be [V, {sh.H}], got {tuple(self.We.shape)}")
+            self.embed_scale = float(embed_scale)
+            self.V = int(self.We.shape[0])
+            self.X0 = torch.empty(T, sh.H, dtype=torch.float16, device=self.dev)
+            self.dWe = torch.empty_like(self.We)
+            self.embed_ws_bytes = lt.lt_embed_bwd_workspace_size(T, sh.H, self.V)
+            self.embed_ws = torch.empty(self.embed_ws_bytes, dtype=torch.uint8, device=self.dev)
         self.opt = None
         if optimizer_state:
-            n = sum(int(x.numel()) for L_ in self.layers for x in (L_.Wqkv, L_.Wo, L_.Wgu, L_.Wd))
-            self.opt = torch.empty(3 * n, dtype=torch.float32, device=self.dev)
+            self.opt = torch.empty(3 * self.params(), dtype=torch.float32, device=self.dev)
 
     def params(self):
-        return sum(int(x.numel()) for L_ in self.layers for x in (L_.Wqkv, L_.Wo, L_.Wgu, L_.Wd))
+        return (sum(int(x.numel()) for L_ in self.layers for x in (L_.Wqkv, L_.Wo, L_.Wgu, L_.Wd)) +
+                (int(self.We.numel()) if self.We is not None else 0))
+
+    def _check_ids(self, ids):
+        if ids.dtype != torch.int64 or ids.numel() != self.X0.shape[0] or not ids.is_contiguous():
+            raise ValueError(f"a micro-batch of this stage is {self.X0.shape[0]} contiguous int64 token ids")
 
     def _forward(self, l, x, stream):
         L_ = self.layers[l]
@@ -76,18 +102,25 @@ class Stage:
         return L_.Y
 
     def forward(self, x, stream=None):
-        """Forward of one micro-batch through the L layers; returns the output."""
+        """Forward of one micro-batch (the layers' input, or with an embedding the token ids)
+        through the L layers; returns the output."""
         y = x
+        if self.We is not None:
+            self._check_ids(x)
+            lt.lt_embed_fwd(x, self.We, self.sh.H, self.embed_scale, self.X0, self.sh.H, x.numel(), self.sh.H, self.V,
+                            stream)
+            y = self.X0
         for l in range(self.L):
             y = self._forward(l, y, stream)
         return y
 
     def backward(self, x, dy, first, stream=None):
         """Backward of the micro-batch whose forward ran last (input x, output
-        gradient dy); returns the input gradient (a view of one of the stage's
-        two gradient buffers).  ``first``: overwrite the weight gradients
-        instead of accumulating."""
+        gradient dy); returns the gradient of the layers' input (a view of one
+        of the stage's two gradient buffers).  ``first``: overwrite the weight
+        gradients instead of accumulating."""
         g = dy
+        ids, x = x, (x if self.We is None else self.X0)
         for l in reversed(range(self.L)):
             L_ = self.layers[l]
             if self.act == "ckpt":
@@ -98,6 +131,10 @@ class Stage:
             L_.accumulate = not first
             L_.backward(stream)
             g = L_.dX
+        if self.We is not None:
+            self._check_ids(ids)
+            lt.lt_embed_bwd(ids, g, self.sh.H, self.embed_scale, 0 if first else 1, self.dWe, self.sh.H,
+                            self.embed_ws, self.embed_ws_bytes, ids.numel(), self.sh.H, self.V, stream)
         return g
 
     def micro_batch(self, x, dy, first, stream=None):

@@ -56,12 +56,16 @@ TENSOR_INDEX = {"X": 0, "dY": 1, "Wqkv": 2, "Wo": 3, "Wgu": 4, "Wd": 5,
 @dataclass(frozen=True)
 class NormInputs:
     """RMSNorm weights [H] of the attention and FFN inputs, eps, rotary base
-    and the QKV projection bias [(Hq + 2 Hkv) d] (Qwen2.5; None for LLaMA-2)."""
+    (None: no rotary embedding, as with a distance bias), the QKV projection
+    bias [(Hq + 2 Hkv) d] (Qwen2.5; None for LLaMA-2) and the RMSNorm weights [d] of
+    every query and key head (None: no QK norm)."""
     wn1: np.ndarray
     wn2: np.ndarray
     eps: float
     rope_base: float
     bqkv: object = None
+    wq: object = None
+    wk: object = None
 
 
 # eps and rotary base of the evaluated model families (their published
