@@ -50,6 +50,27 @@ struct Score {
   }
 };
 
+// With a distance bias most pairs of a steep head have no weight: their
+// probability is a zero in FP16.  Where that holds for a whole tile of a wave, what
+// follows the scores is left out:
+//   * forward: probabilities below 2^-kNoneFwd of the row's offset; all such of a row
+//     (at most 2^19 keys) are below half a step of its FP32 sum, which is at least 1;
+//   * backward: below 2^-kNoneBwd, so that dS is an FP16 zero too, whatever dP - D is
+//     (|dP| <= 128 * 65504^2 < 2^39).
+// So the results are the same; only a non-finite V or dO behind such a weight is not
+// seen.  Non-finite scores are never left out.
+constexpr float kNoneFwd = 48.f;
+constexpr float kNoneBwd = 66.f;
+template <int N>
+__device__ __forceinline__ bool all_finite(const f32x16 (&acc)[N]) {
+  float m = 0.f;   // 0, or NaN
+#pragma unroll
+  for (int kb = 0; kb < N; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) m = fmaf(acc[kb][r], 0.f, m);
+  return __builtin_amdgcn_ballot_w64(!(m == 0.f)) == 0;
+}
+
 // Values -slope' |d0 + n| of a 32-wide accumulator column, n = 8 (r / 4) + r % 4, r < 16,
 // step by step of kb (32 more).  `side`: every d0 + n of the wave has that sign (+1, -1),
 // or 0: mixed.  With a sign the value is linear in n: one add of a scalar each.
@@ -76,15 +97,6 @@ __device__ __forceinline__ void bias_init(f32x16 (&acc)[N], float slope, float d
 // non-finite V, K, Q or dO.  The kernels pay nothing for that case on the way: where an
 // accumulator of a wave ends up non-finite, they form it again one (query, key) pair at a time,
 // over the pairs that see each other.
-template <int DB>
-__device__ __forceinline__ bool all_finite(const f32x16 (&acc)[DB]) {
-  float m = 0.f;
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) m = fmaf(acc[db][r], 0.f, m);     // 0, or NaN
-  return __builtin_amdgcn_ballot_w64(!(m == 0.f)) == 0;
-}
 // this lane's half of a row product: features kk * 16 + 8 g + 0..7 of both
 template <int KK>
 __device__ __forceinline__ float half_dot(const half8 (&f)[KK], const lt_half* row) {

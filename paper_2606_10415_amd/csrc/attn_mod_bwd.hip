@@ -34,7 +34,8 @@ namespace lt {
 namespace {
 
 // Direct load of 16 bytes per lane into LDS, as lds_dma16_opaque, for data
-// read once (non-temporal).
+// read once (non-temporal).  The wait states cover a descriptor word that a
+// v_readfirstlane has just written as well as m0.
 __device__ __forceinline__ void lds_dma16_stream(const void* base, uint32_t nrec, void* lds, uint32_t voff) {
   const uint64_t b = (uint64_t)base;
   u32x4 r;
@@ -43,7 +44,7 @@ __device__ __forceinline__ void lds_dma16_stream(const void* base, uint32_t nrec
   r[2] = __builtin_amdgcn_readfirstlane(nrec);
   r[3] = 0x00020000u;
   const uint32_t m0v = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
                :
                : "s"(m0v), "v"(voff), "s"(r)
                : "memory");
@@ -54,7 +55,10 @@ constexpr int BKV = NWA * 32;  // dK/dV: keys per workgroup (32 per wave)
 constexpr int BQA = 64;        // dK/dV: queries per block (two 32-query halves)
 constexpr int kMaxBlocks = kModMaxS / BQA;
 
-// dS block (query group qg, key group kg) of a head
+// dS blocks of a head; block (query group qg, key group kg)
+__device__ __forceinline__ int64_t ds_blocks(int n32, int causal) {
+  return causal ? (int64_t)n32 * (n32 + 1) / 2 : (int64_t)n32 * n32;
+}
 __device__ __forceinline__ int64_t ds_block(int qg, int kg, int n32, int causal) {
   return causal ? (int64_t)qg * (qg + 1) / 2 + kg : (int64_t)qg * n32 + kg;
 }
@@ -269,48 +273,69 @@ attn_mod_delta_kernel(const AttnModBwdArgs a, int all, unsigned n_tile) {
         return as_half8(*reinterpret_cast<const u32x4*>(st + off + (kb0 + kb * 32) * RT::ROWB + rlane[kk]));
       };
       half8 kfr[2][KBW], vfr[2][KBW];
-#pragma unroll
-      for (int kb = 0; kb < KBW; ++kb) {
-        kfr[0][kb] = rd(0, kb, 0);
-        vfr[0][kb] = rd(TILE, kb, 0);
-      }
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        if (kk + 1 < KK) {
-#pragma unroll
-          for (int kb = 0; kb < KBW; ++kb) {
-            kfr[(kk + 1) & 1][kb] = rd(0, kb, kk + 1);
-            vfr[(kk + 1) & 1][kb] = rd(TILE, kb, kk + 1);
-          }
-        }
+      const bool full = key0 >= wh.all_lo && key0 + KBW * 32 <= wh.all_hi;      // wave-uniform
+      // scores (with a distance bias first, to see whether they have any weight), then dP
+      auto products = [&](auto S_, auto P_) __attribute__((always_inline)) {
+        constexpr bool WS = decltype(S_)::value, WP = decltype(P_)::value;
 #pragma unroll
         for (int kb = 0; kb < KBW; ++kb) {
-          sacc[kb] = mfma32(kfr[kk & 1][kb], qf[kk], sacc[kb]);
-          pacc[kb] = mfma32(vfr[kk & 1][kb], gf[kk], pacc[kb]);
+          if (WS) kfr[0][kb] = rd(0, kb, 0);
+          if (WP) vfr[0][kb] = rd(TILE, kb, 0);
         }
-      }
-      const bool full = key0 >= wh.all_lo && key0 + KBW * 32 <= wh.all_hi;      // wave-uniform
 #pragma unroll
-      for (int kb = 0; kb < KBW; ++kb)
+        for (int kk = 0; kk < KK; ++kk) {
+          if (kk + 1 < KK) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float t = sc.t(sacc[kb][r]);
-          if constexpr (CAP && BIAS) t = fmaf(-slope, fabsf(d0 + (float)(kb * 32 + 8 * (r >> 2) + (r & 3))), t);
-          sacc[kb][r] = fast_exp2(fmaf(t, sc.c, -lse2)) * pacc[kb][r];
+            for (int kb = 0; kb < KBW; ++kb) {
+              if (WS) kfr[(kk + 1) & 1][kb] = rd(0, kb, kk + 1);
+              if (WP) vfr[(kk + 1) & 1][kb] = rd(TILE, kb, kk + 1);
+            }
+          }
+#pragma unroll
+          for (int kb = 0; kb < KBW; ++kb) {
+            if (WS) sacc[kb] = mfma32(kfr[kk & 1][kb], qf[kk], sacc[kb]);
+            if (WP) pacc[kb] = mfma32(vfr[kk & 1][kb], gf[kk], pacc[kb]);
+          }
         }
-      if (!full) {
+      };
+      bool none = false;
+      if constexpr (BIAS) products(std::true_type{}, std::false_type{});
+      else products(std::true_type{}, std::true_type{});
+      if constexpr (CAP || BIAS) {
+        float mx = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < KBW; ++kb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int key = key0 + kb * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-            sacc[kb][r] = ((key >= lo) & (key < hi)) ? sacc[kb][r] : 0.f;
+            sacc[kb][r] = sc.t(sacc[kb][r]);
+            if constexpr (CAP && BIAS)
+              sacc[kb][r] = fmaf(-slope, fabsf(d0 + (float)(kb * 32 + 8 * (r >> 2) + (r & 3))), sacc[kb][r]);
+            if constexpr (BIAS) mx = fmaxf(mx, sacc[kb][r]);
           }
+        if constexpr (BIAS) {
+          none = full && __builtin_amdgcn_ballot_w64(!(fmaf(mx, sc.c, -lse2) < -kNoneBwd)) == 0 && all_finite(sacc);
+          if (!none) products(std::false_type{}, std::true_type{});
+        }
       }
+      if (!none) {
 #pragma unroll
-      for (int kb = 0; kb < KBW; ++kb)
+        for (int kb = 0; kb < KBW; ++kb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dex += sacc[kb][r];
+          for (int r = 0; r < 16; ++r) sacc[kb][r] = fast_exp2(fmaf(sacc[kb][r], sc.c, -lse2)) * pacc[kb][r];
+        if (!full) {
+#pragma unroll
+          for (int kb = 0; kb < KBW; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int key = key0 + kb * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
+              sacc[kb][r] = ((key >= lo) & (key < hi)) ? sacc[kb][r] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int kb = 0; kb < KBW; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) dex += sacc[kb][r];
+      }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -384,6 +409,7 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
   const int kvh = (bkv0 + lbkv) % Hkv;
   const int G = Hq / Hkv;
   const int n32 = (S + 31) / 32;
+  const int64_t nblk = ds_blocks(n32, causal);
   const int kbase = jt * BK;
   const int kw0 = kbase + kg * 32;                 // this wave's first key
   const int mykey = kw0 + lrow;                    // key owned by this lane (S, dP columns)
@@ -548,27 +574,75 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
           asm volatile("v_add_u32 %0, %1, %2" : "=v"(ad) : "v"(rlane[kk]), "s"(vrow0));
           return as_half8(*reinterpret_cast<const u32x4*>(smem + ad));
         };
-        half8 fq = rdq(0);
-        half8 fd = rdo(0);
-        half8 fv = rdv(0);
-        __builtin_amdgcn_s_setprio(1);
+        char* const dsb = reinterpret_cast<char*>(a.ds) +
+                          (((int64_t)lbkv * G + j) * nblk + ds_block(qh >> 5, kw0 >> 5, n32, causal)) * kDsBlockBytes;
+        uint8_t* const live = a.live + ((int64_t)lbkv * G + j) * nblk + ds_block(qh >> 5, kw0 >> 5, n32, causal);
+        const bool full = kw0 >= all_lo && kw0 + 32 <= all_hi;     // wave-uniform
+        half8 fd, fv;
+        if constexpr (BIAS) {
+          // the scores first, to see whether the block has any weight (kNoneBwd)
+          half8 fq = rdq(0);
+          __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          half8 nq = fq, nd = fd, nv = fv;
-          if (kk + 1 < KK) {
-            nq = rdq(kk + 1);
-            nd = rdo(kk + 1);
-            nv = rdv(kk + 1);
+          for (int kk = 0; kk < KK; ++kk) {
+            half8 nq = fq;
+            if (kk + 1 < KK) nq = rdq(kk + 1);
+            sacc = mfma32(fq, kf[kk], sacc);
+            fq = nq;
           }
-          sacc = mfma32(fq, kf[kk], sacc);
-          pacc = mfma32(fd, fv, pacc);
-          if (kk + 1 < KK) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);   // the three reads
-            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);   // then the two MFMAs
+          __builtin_amdgcn_s_setprio(0);
+          float mx = -INFINITY;
+#pragma unroll
+          for (int rq = 0; rq < 4; ++rq) {
+            const float4 l4 = *reinterpret_cast<const float4*>(lse_s + hq * 32 + 8 * rq + 4 * g);
+            const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float t = sc.t(sacc[4 * rq + e]);
+              if constexpr (CAP) t = fmaf(-slope, fabsf(d0 + (float)(8 * rq + e)), t);
+              mx = fmaxf(mx, fmaf(t, sc.c, -lv[e]));
+            }
           }
-          fq = nq;
-          fd = nd;
-          fv = nv;
+          const bool none = full && __builtin_amdgcn_ballot_w64(!(mx < -kNoneBwd)) == 0 && all_finite(sacc1);
+          if (lane == 0) *live = !none;
+          if (none) return;
+          fd = rdo(0);
+          fv = rdv(0);
+          __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk) {
+            half8 nd = fd, nv = fv;
+            if (kk + 1 < KK) {
+              nd = rdo(kk + 1);
+              nv = rdv(kk + 1);
+            }
+            pacc = mfma32(fd, fv, pacc);
+            fd = nd;
+            fv = nv;
+          }
+        } else {
+          half8 fq = rdq(0);
+          fd = rdo(0);
+          fv = rdv(0);
+          __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk) {
+            half8 nq = fq, nd = fd, nv = fv;
+            if (kk + 1 < KK) {
+              nq = rdq(kk + 1);
+              nd = rdo(kk + 1);
+              nv = rdv(kk + 1);
+            }
+            sacc = mfma32(fq, kf[kk], sacc);
+            pacc = mfma32(fd, fv, pacc);
+            if (kk + 1 < KK) {
+              __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);   // the three reads
+              __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);   // then the two MFMAs
+            }
+            fq = nq;
+            fd = nd;
+            fv = nv;
+          }
         }
         __builtin_amdgcn_s_setprio(0);
         // P = exp2(c t - LSE2), dS = P (dP - D) (1 - tanh^2)
@@ -595,7 +669,7 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] *= p[r];
-        if (kw0 < all_lo || kw0 + 32 > all_hi) {   // wave-uniform: some query sees them in part
+        if (!full) {                               // some query sees them in part
 #pragma unroll
           for (int rq = 0; rq < 4; ++rq) {
             const int ql0 = hq * 32 + 8 * rq + 4 * g;
@@ -622,10 +696,7 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
         // dS block for the dQ pass, as held here (lane-major, 32 bytes per
         // lane); written once, read once: non-temporal
         {
-          const int64_t nblk = causal ? (int64_t)n32 * (n32 + 1) / 2 : (int64_t)n32 * n32;
-          char* dst = reinterpret_cast<char*>(a.ds) +
-                      (((int64_t)lbkv * G + j) * nblk + ds_block(qh >> 5, kw0 >> 5, n32, causal)) * kDsBlockBytes +
-                      lane * 32;
+          char* dst = dsb + lane * 32;
           __builtin_nontemporal_store(as_u32x4(pds[0]), reinterpret_cast<u32x4*>(dst));
           __builtin_nontemporal_store(as_u32x4(pds[1]), reinterpret_cast<u32x4*>(dst + 16));
         }
@@ -854,7 +925,9 @@ __device__ __forceinline__ void wait_vmcnt() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-template <int D, int NWQ>
+// MARKS (with a distance bias): only the blocks that their marks call live are read, and
+// only slices that some wave of the workgroup has one in.
+template <int D, int NWQ, bool MARKS>
 __global__ void __launch_bounds__(NWQ * 64, 1)
 attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
   using SM = DqSmem<D, NWQ>;
@@ -899,10 +972,10 @@ attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
   kg0 = __builtin_amdgcn_readfirstlane(kg0);
   kg_end = __builtin_amdgcn_readfirstlane(kg_end);
   const int ks0 = __builtin_amdgcn_readfirstlane(wg_lo < wg_hi ? wg_lo / BKQ : 0);
-  const int n_ks = __builtin_amdgcn_readfirstlane(wg_lo < wg_hi ? (wg_hi + BKQ - 1) / BKQ - ks0 : 0);
+  const int ks1 = __builtin_amdgcn_readfirstlane(wg_lo < wg_hi ? (wg_hi + BKQ - 1) / BKQ : 0);
 
   const lt_half* Kp = a.K + (int64_t)b * S * a.kv_stride + (int64_t)kvh * D;
-  const int64_t nblk = causal ? (int64_t)n32 * (n32 + 1) / 2 : (int64_t)n32 * n32;
+  const int64_t nblk = ds_blocks(n32, causal);
   // block (qg, 0); block (qg, kg) follows at kg * 2 KiB
   const char* dsq = reinterpret_cast<const char*>(a.ds) +
                     (((int64_t)lbkv * G + j) * nblk + ds_block(qg < n32 ? qg : 0, 0, n32, causal)) * kDsBlockBytes;
@@ -913,21 +986,71 @@ attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
 
-  // slice i (keys from (ks0 + i) * 64) -> stage i % NSQ; K rows past S read as zero
-  auto stage = [&](int i) {
-    char* st = smem + (i % NSQ) * SM::STAGE;
-    const int ks = ks0 + i;
+  // live blocks of 64 key groups (32 slices) from 64 win: this wave's, any wave's
+  int win = -1;
+  uint64_t mine_w = 0, any_w = 0;
+  auto load_window = [&](int w) {
+    win = w;
+    const int kg = w * 64 + lane;
+    bool mine = false, any = false;
+#pragma unroll
+    for (int u = 0; u < NWQ; ++u) {
+      const int q = qt * NWQ + u;
+      if (q >= n32) continue;
+      const QueryHull hu = hulls[q];
+      const bool on = hu.lo < hu.hi && kg >= hu.lo >> 5 && kg < (hu.hi + 31) >> 5 &&
+                      a.live[((int64_t)lbkv * G + j) * nblk + ds_block(q, kg, n32, causal)];
+      any |= on;
+      if (u == wave) mine = on;
+    }
+    mine_w = __builtin_amdgcn_ballot_w64(mine);
+    any_w = __builtin_amdgcn_ballot_w64(any);
+  };
+  // the next slice from ks on to go through (ks1: none), and this wave's two blocks of it
+  auto next_slice = [&](int ks, uint32_t& own) {
+    if constexpr (!MARKS) {
+      own = (2 * ks >= kg0 && 2 * ks < kg_end ? 1 : 0) | (2 * ks + 1 >= kg0 && 2 * ks + 1 < kg_end ? 2 : 0);
+      return ks;
+    }
+    for (; ks < ks1; ks = (win + 1) * 32) {
+      if (ks >> 5 != win) load_window(ks >> 5);
+      const uint64_t left = any_w >> (2 * (ks & 31));
+      if (left) {
+        ks += __builtin_ctzll(left) >> 1;
+        own = (uint32_t)(mine_w >> (2 * (ks & 31))) & 3;
+        return ks;
+      }
+    }
+    return ks1;
+  };
+
+  // the staged-th slice (keys from ks * 64) -> stage staged % NSQ; K rows past S read
+  // as zero.  owns: two bits a stage, which of the wave's blocks are there
+  int staged = 0;
+  uint32_t owns = 0, own = 0;
+  int ks = ks1;
+  auto advance = [&](int from) {
+    ks = __builtin_amdgcn_readfirstlane(from < ks1 ? next_slice(from, own) : ks1);
+    own = __builtin_amdgcn_readfirstlane(own);
+  };
+  advance(ks0);
+  auto stage_next = [&] {
+    if (ks >= ks1) return;
+    const int slot = staged % NSQ;
+    char* st = smem + slot * SM::STAGE;
     RT::template dma<BKQ>(st, Kp + (int64_t)ks * BKQ * a.kv_stride, a.kv_stride, S - ks * BKQ, wave, lane);
     char* mine = st + SM::KT + wave * SM::DSW;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const int kg = 2 * ks + c;
-      const bool in = kg >= kg0 && kg < kg_end;
-      const char* src = dsq + (int64_t)(in ? kg : 0) * kDsBlockBytes;
+      const bool in = own >> c & 1;
+      const char* src = dsq + (int64_t)(in ? 2 * ks + c : 0) * kDsBlockBytes;
       const uint32_t nrec = in ? kDsBlockBytes : 0u;
       lds_dma16_stream(src, nrec, mine + c * kDsBlockBytes, (uint32_t)(lane * 16));
       lds_dma16_stream(src, nrec, mine + c * kDsBlockBytes + 1024, (uint32_t)(1024 + lane * 16));
     }
+    owns = __builtin_amdgcn_readfirstlane((owns & ~(3u << (2 * slot))) | own << (2 * slot));
+    ++staged;
+    advance(ks + 1);
   };
 
   // slices after the next one may stay in flight, up to NSQ - 2 of them
@@ -936,18 +1059,19 @@ attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
     else if (NSQ > 3 && behind == 1) wait_vmcnt<SM::LOADS>();
     else wait_vmcnt<0>();
   };
-  for (int i = 0; i < NSQ - 1 && i < n_ks; ++i) stage(i);
-  wait_next(min(NSQ - 1, n_ks) - 1);               // slice 0 resident
+#pragma unroll
+  for (int i = 0; i < NSQ - 1; ++i) stage_next();
+  wait_next(staged - 1);                           // slice 0 resident
   __syncthreads();
-  for (int i = 0; i < n_ks; ++i) {
+  for (int i = 0; i < staged; ++i) {
     // the stage of slice i + NSQ - 1 was last read before the previous barrier
-    if (i + NSQ - 1 < n_ks) stage(i + NSQ - 1);
+    stage_next();
     const char* st = smem + (i % NSQ) * SM::STAGE;
     const char* mine = st + SM::KT + wave * SM::DSW;
+    const uint32_t now = owns >> (2 * (i % NSQ));
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const int kg = 2 * (ks0 + i) + c;
-      if (kg >= kg0 && kg < kg_end) {
+      if (now >> c & 1) {
 #pragma unroll
         for (int kc = 0; kc < 2; ++kc) {
           //   dQ^T += K^T dS^T  (K^T read transposed, keys in accumulator order)
@@ -960,7 +1084,7 @@ attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
     }
     // the next slice resident for every wave (later slices' loads may still be
     // in flight); nobody reads this stage any more
-    wait_next(min(i + NSQ - 1, n_ks - 1) - (i + 1));
+    wait_next(staged - (i + 2));
     __syncthreads();
   }
 
@@ -978,6 +1102,7 @@ attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
       row_interval(a.mod, causal, b, S, q, lo, hi);
 #pragma nounroll
       for (int k = kg0 * 32; k < min(kg_end * 32, S); ++k) {
+        if (MARKS && !a.live[((int64_t)lbkv * G + j) * nblk + ds_block(qg, k >> 5, n32, causal)]) continue;
         const char* el = dsq + (int64_t)(k >> 5) * kDsBlockBytes + ((k & 31) + 32 * (pos >> 4)) * 32 + (pos & 15) * 2;
         add_row(acc, (k >= lo) & (k < hi), (float)*reinterpret_cast<const _Float16*>(el),
                 Kp + (int64_t)k * a.kv_stride, g);
@@ -1046,7 +1171,7 @@ hipError_t launch_bwd(const AttnModBwdArgs& a, hipStream_t s) {
     auto launch_dq = [&](auto W_) {
       constexpr int NWQ = decltype(W_)::value;
       const int n_qt = (sh.S + NWQ * 32 - 1) / (NWQ * 32);
-      hipLaunchKernelGGL((attn_mod_dq_kernel<D, NWQ>), dim3((unsigned)((int64_t)n_qt * nb * grp)), dim3(NWQ * 64), 0,
+      hipLaunchKernelGGL((attn_mod_dq_kernel<D, NWQ, BIAS>), dim3((unsigned)((int64_t)n_qt * nb * grp)), dim3(NWQ * 64), 0,
                          s, a, bkv0, nb);
     };
     if ((int64_t)((sh.S + 255) / 256) * nb * grp > kDqHalfWgs) launch_dq(std::integral_constant<int, 8>{});

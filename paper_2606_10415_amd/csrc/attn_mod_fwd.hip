@@ -131,7 +131,7 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
     RT::template dma<BKV>(st, Kp + (int64_t)key0 * kv_stride, kv_stride, S - key0, wave, lane);
     RT::template dma<BKV>(st + SM::TILE, Vp + (int64_t)key0 * kv_stride, kv_stride, S - key0, wave, lane);
   };
-  if (kt0 < kt1) stage_load(kt0, 0);
+  if (kt0 < kt1) stage_load(kt1 - 1, 0);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
 
@@ -141,7 +141,7 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
     constexpr int cur = decltype(CUR_)::value;
     const char* st = smem + cur * SM::STAGE;
     // that stage was last read before the previous barrier
-    if (kt + 1 < kt1) stage_load(kt + 1, cur ^ 1);
+    if (kt > kt0) stage_load(kt - 1, cur ^ 1);
 
     const int kb0 = QSPLIT > 1 ? kpart * 32 : 0;
     const int key0 = kt * BKV + kb0;               // this wave's keys: KBW * 32 from here
@@ -199,7 +199,8 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
       }
 
       // ---- mask, row max ----
-      if (key0 < wh.all_lo || key0 + KBW * 32 > wh.all_hi) {       // wave-uniform
+      const bool partly = key0 < wh.all_lo || key0 + KBW * 32 > wh.all_hi;   // wave-uniform
+      if (partly) {
 #pragma unroll
         for (int kb = 0; kb < KBW; ++kb)
 #pragma unroll
@@ -214,6 +215,10 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[kb][r]);
       mx = fmaxf(mx, __shfl_xor(mx, 32));
+      // a slice of no weight ends here (kNoneFwd); the slices run from the last, so that a
+      // causal row has its nearest keys, and its maximum, first
+      const bool none = BIAS && !partly && __builtin_amdgcn_ballot_w64(!(mx < m_run - kNoneFwd / c)) == 0 &&
+                        all_finite(sacc);
 
       // ---- raise the running max only past the lazy margin ----
       const bool raise = mx > m_run + lazy_raw;    // m_run = -inf until the query's first key
@@ -230,41 +235,43 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
 
       // ---- P = exp2(z - m), row sum, FP16 P^T fragments ----
       // (a query without a key so far: every score is -inf, P = exp2(-inf) = 0)
-      const float mc = m_run == -INFINITY ? 0.f : m_run * c;
-      half8 pf[KBW][2];
+      if (!none) {
+        const float mc = m_run == -INFINITY ? 0.f : m_run * c;
+        half8 pf[KBW][2];
 #pragma unroll
-      for (int kb = 0; kb < KBW; ++kb) {
-        float p[16];
+        for (int kb = 0; kb < KBW; ++kb) {
+          float p[16];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          p[r] = fast_exp2(fmaf(sacc[kb][r], c, -mc));
-          lsum += p[r];
+          for (int r = 0; r < 16; ++r) {
+            p[r] = fast_exp2(fmaf(sacc[kb][r], c, -mc));
+            lsum += p[r];
+          }
+#pragma unroll
+          for (int kc = 0; kc < 2; ++kc)
+            pf[kb][kc] = pack8(p[8 * kc + 0], p[8 * kc + 1], p[8 * kc + 2], p[8 * kc + 3],
+                               p[8 * kc + 4], p[8 * kc + 5], p[8 * kc + 6], p[8 * kc + 7]);
         }
-#pragma unroll
-        for (int kc = 0; kc < 2; ++kc)
-          pf[kb][kc] = pack8(p[8 * kc + 0], p[8 * kc + 1], p[8 * kc + 2], p[8 * kc + 3],
-                             p[8 * kc + 4], p[8 * kc + 5], p[8 * kc + 6], p[8 * kc + 7]);
-      }
 
-      // ---- O^T += V^T P^T (V^T read transposed, keys in accumulator order) ----
-      const char* vs = st + SM::TILE;
+        // ---- O^T += V^T P^T (V^T read transposed, keys in accumulator order) ----
+        const char* vs = st + SM::TILE;
 #pragma unroll
-      for (int kb = 0; kb < KBW; ++kb)
+        for (int kb = 0; kb < KBW; ++kb)
 #pragma unroll
-        for (int kc = 0; kc < 2; ++kc)
+          for (int kc = 0; kc < 2; ++kc)
 #pragma unroll
-          for (int db = 0; db < DB; ++db)
-            oacc[db] = mfma32(RT::template tr_frag<true>(vs, kb0 + kb * 32 + kc * 16, db * 32, lane), pf[kb][kc],
-                              oacc[db]);
+            for (int db = 0; db < DB; ++db)
+              oacc[db] = mfma32(RT::template tr_frag<true>(vs, kb0 + kb * 32 + kc * 16, db * 32, lane), pf[kb][kc],
+                                oacc[db]);
+      }
     }
 
     // next slice resident for every wave; nobody reads this stage any more
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
-  for (int kt = kt0; kt < kt1; kt += 2) {
+  for (int kt = kt1 - 1; kt >= kt0; kt -= 2) {
     slice(kt, std::integral_constant<int, 0>{});
-    if (kt + 1 < kt1) slice(kt + 1, std::integral_constant<int, 1>{});
+    if (kt > kt0) slice(kt - 1, std::integral_constant<int, 1>{});
   }
 
   if constexpr (QSPLIT > 1) {

@@ -163,7 +163,8 @@ __device__ __forceinline__ int64_t part_row(int p, int k) { return 2 * (int64_t)
 
 // Workgroups 0 .. parts x ncb - 1: (kEmbedPart positions, 2048 columns).  They take the
 // runs, and the pieces of long runs, that start in their positions: at most
-// 2 kEmbedPart - 1 tokens.  The others: a wave per row, zeros where no token falls.
+// 2 kEmbedPart - 1 tokens.  The others: a wave per row, zeros where no token falls
+// (non-temporal, so that they do not evict the tokens' rows; more rows a wave: level).
 __global__ void __launch_bounds__(kThreads)
 embed_walk_kernel(const EmbedBwdArgs a, int parts, int ncb) {
   constexpr int C = kEmbedPart;
@@ -172,7 +173,8 @@ embed_walk_kernel(const EmbedBwdArgs a, int parts, int ncb) {
   if (blockIdx.x >= (unsigned)(parts * ncb)) {
     const int64_t v = (int64_t)(blockIdx.x - parts * ncb) * kRowWaves + (threadIdx.x >> 6);
     if (v >= a.V || a.start[v] != a.start[v + 1]) return;
-    for (int64_t col = lane * 8; col < a.H; col += 64 * 8) st16(a.dW + v * a.lddw + col, u32x4{0, 0, 0, 0});
+    for (int64_t col = lane * 8; col < a.H; col += 64 * 8)
+      __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4*>(a.dW + v * a.lddw + col));
     return;
   }
   const int n = a.start[a.V];

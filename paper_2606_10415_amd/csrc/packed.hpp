@@ -92,10 +92,11 @@ inline AttnModPlan attn_mod_plan(int B, int S, int Hq, int Hkv, int D, int causa
 // Workspace parts of the backward, in order, each 256-byte aligned: D and the
 // base-2 LSE [B, Hq, S] FP32, the rows' intervals [2][B, S] and the hulls
 // [B][ceil(S / 32)], a bit for every query of a head (tiles of kSharpTile), one chunk's
-// dS blocks, one chunk's partial dK and dV.
+// dS blocks and, with a distance bias, a byte for each of them, one chunk's
+// partial dK and dV.
 constexpr int kSharpTile = 128;
 struct AttnModWs {
-  size_t lse2, rows, hulls, sharp, ds, part, total;
+  size_t lse2, rows, hulls, sharp, ds, live, part, total;
 };
 inline AttnModWs attn_mod_ws(int B, int S, int Hq, int Hkv, int D, int causal) {
   const AttnModPlan p = attn_mod_plan(B, S, Hq, Hkv, D, causal);
@@ -106,7 +107,9 @@ inline AttnModWs attn_mod_ws(int B, int S, int Hq, int Hkv, int D, int causal) {
   w.hulls = w.rows + align256((size_t)2 * B * S * sizeof(int32_t));
   w.sharp = w.hulls + align256((size_t)B * n32 * sizeof(QueryHull));
   w.ds = w.sharp + align256((size_t)B * Hq * (((size_t)S + kSharpTile - 1) / kSharpTile) * (kSharpTile / 8));
-  w.part = w.ds + align256((size_t)p.chunk * (Hq / Hkv) * (size_t)attn_bwd_ds_blocks(S, causal) * kDsBlockBytes);
+  const size_t blocks = (size_t)p.chunk * (Hq / Hkv) * (size_t)attn_bwd_ds_blocks(S, causal);
+  w.live = w.ds + align256(blocks * kDsBlockBytes);
+  w.part = w.live + align256(blocks);
   w.total = w.part + (p.nsplit > 1 ? align256((size_t)2 * p.chunk * p.nsplit * S * D * sizeof(float)) : 0);
   return w;
 }
@@ -133,6 +136,7 @@ struct AttnModBwdArgs {
   QueryHull* hulls;
   uint32_t* sharp;
   lt_half* ds;
+  uint8_t* live;          // 0: the block is all zeros and was not written
   float* part;
 };
 

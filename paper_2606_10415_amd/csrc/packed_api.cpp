@@ -175,6 +175,7 @@ lt_status lt_attn_mod_bwd(const lt_half* Q, const lt_half* K, const lt_half* V, 
                        reinterpret_cast<lt::QueryHull*>(ws + w.hulls),
                        reinterpret_cast<uint32_t*>(ws + w.sharp),
                        reinterpret_cast<lt_half*>(ws + w.ds),
+                       reinterpret_cast<uint8_t*>(ws + w.live),
                        reinterpret_cast<float*>(ws + w.part)};
   return from_hip(lt::attn_mod_bwd_launch(a, reinterpret_cast<hipStream_t>(stream)), "attn_mod_bwd launch");
 }
