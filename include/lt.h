@@ -454,7 +454,9 @@ lt_status lt_rope_f16(lt_half* X, int64_t row_stride, int B, int S, int heads,
  *   LO = i - width + 1, causal = 1.  A padded batch: HI = the row's length, and
  *   HI = 0 for the padding.  A query that sees no key gets O = 0 and LSE = -inf.
  *   Non-finite values reach only those that see them: keys that no query sees and
- *   queries that see nothing may hold anything (slower where they do).
+ *   queries that see nothing may hold anything (slower where they do).  With
+ *   slopes, tiles whose probabilities are all below 2^-48 of their row's largest
+ *   are left out: zeros in FP16, below the rounding of the row's FP32 sum.
  *   slopes: [Hq] FP32 device array or NULL.  cap: 0 for none, else up to 1000.
  *   Layouts, head grouping and errors as lt_attn_fwd, and
  *   LT_ERR_INVALID_ARG for a cap that is negative or not finite;

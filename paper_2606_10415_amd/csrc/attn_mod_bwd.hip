@@ -54,6 +54,9 @@ constexpr int NWA = 8;         // dK/dV: waves per workgroup
 constexpr int BKV = NWA * 32;  // dK/dV: keys per workgroup (32 per wave)
 constexpr int BQA = 64;        // dK/dV: queries per block (two 32-query halves)
 constexpr int kMaxBlocks = kModMaxS / BQA;
+// marks of dS blocks (with a distance bias): 0 no weight, found before the dK/dV pass,
+// which then does not visit the block; kZeroBlock none either, found by that pass
+constexpr uint8_t kLiveBlock = 1, kZeroBlock = 2;
 
 // dS blocks of a head; block (query group qg, key group kg)
 __device__ __forceinline__ int64_t ds_blocks(int n32, int causal) {
@@ -156,6 +159,7 @@ attn_mod_rows_kernel(const AttnModBwdArgs a, unsigned n_tile) {
 // of their sharp queries.  `all` (short sequences, where another launch costs more than
 // these products): every query is taken, the base-2 LSE is written too, and the
 // workgroups from n_tile on do the intervals and hulls, in place of attn_mod_rows.
+// With a distance bias the pass also says which dS blocks have any weight.
 constexpr int NWD = 4;            // waves
 constexpr int BKD = 64;           // keys per slice
 
@@ -178,7 +182,7 @@ attn_mod_delta_kernel(const AttnModBwdArgs a, int all, unsigned n_tile) {
   int b, h;
   query_head(blockIdx.x % (B * Hq), B, Hq, Hkv, b, h);
   const uint32_t* marks = a.sharp + ((int64_t)b * Hq + h) * ((S + kTile - 1) / kTile) * (kTile / 32) + qt * NQG;
-  if (!all) {
+  if (!all && !BIAS) {
     uint32_t any = 0;
 #pragma unroll
     for (int w = 0; w < NQG; ++w) any |= marks[w];
@@ -203,8 +207,21 @@ attn_mod_delta_kernel(const AttnModBwdArgs a, int all, unsigned n_tile) {
     a.delta[ri] = 0.f;                             // kept by queries that see nothing
   }
   int lo = 0, hi = 0;
-  if (all || (marks[qg] >> lrow & 1)) row_interval(a.mod, causal, b, S, myq, lo, hi);
-  const QueryHull wh = query_hull(lo, hi, myq < S);
+  const uint32_t sharp = all ? ~0u : (uint32_t)__builtin_amdgcn_readfirstlane(qw0 < S ? marks[qg] : 0);
+  if (BIAS || (sharp >> lrow & 1)) row_interval(a.mod, causal, b, S, myq, lo, hi);
+  QueryHull wh = query_hull(lo, hi, myq < S);
+  // with a distance bias: a group is taken whole or not at all, and finds which of its
+  // dS blocks have any weight (kNoneBwd); a group that is not taken calls them live
+  const int g32 = qt * NQG + qg;
+  uint8_t* const live = a.live + ((int64_t)b * Hq + h) * ds_blocks((S + 31) / 32, causal) +
+                        ds_block(qw0 < S ? g32 : 0, 0, (S + 31) / 32, causal);
+  const int kg_lo = wh.lo < wh.hi ? wh.lo >> 5 : 0, kg_hi = wh.lo < wh.hi ? (wh.hi + 31) >> 5 : 0;
+  if (BIAS && sharp == 0) {
+    if (kpart == 0)
+      for (int kg = kg_lo + lane; kg < kg_hi; kg += 64) live[kg] = kLiveBlock;
+    wh.lo = 0x7fffffff;
+    wh.hi = 0;
+  }
   if (lane == 0) {
     hull_s[0][wave] = wh.lo;
     hull_s[1][wave] = wh.hi;
@@ -314,6 +331,8 @@ attn_mod_delta_kernel(const AttnModBwdArgs a, int all, unsigned n_tile) {
           }
         if constexpr (BIAS) {
           none = full && __builtin_amdgcn_ballot_w64(!(fmaf(mx, sc.c, -lse2) < -kNoneBwd)) == 0 && all_finite(sacc);
+          const int kg = (key0 >> 5) + lane;
+          if (lane < KBW && kg >= kg_lo && kg < kg_hi) live[kg] = none ? 0 : kLiveBlock;
           if (!none) products(std::false_type{}, std::true_type{});
         }
       }
@@ -352,7 +371,7 @@ attn_mod_delta_kernel(const AttnModBwdArgs a, int all, unsigned n_tile) {
     if (kpart == 1) return;
     dex += red[qg * 64 + lane];
   }
-  if (myq < S && g == 0 && lo < hi) a.delta[ri] = dex;
+  if (myq < S && g == 0 && lo < hi && sharp != 0) a.delta[ri] = dex;
 }
 
 // ------------------------------------------------------------ 2: dK/dV
@@ -427,19 +446,29 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
     kf[kk] = mykey < S ? as_half8(ld16(Kp + (int64_t)mykey * a.kv_stride + kk * 16 + g * 8))
                        : as_half8(u32x4{0, 0, 0, 0});
 
-  // ---- list the tile's query blocks, ascending ----
+  // ---- list the tile's query blocks, ascending; with a distance bias and room for
+  // them the (query head, block) pairs, of those that have a live dS block ----
   const int n_qb = (S + BQA - 1) / BQA;
+  const bool pairs = BIAS && (int64_t)G * n_qb <= kMaxBlocks;
+  const int n_cand = pairs ? G * n_qb : n_qb;
   int n_list = 0;
-  for (int i0 = 0; i0 < n_qb; i0 += NWA * 64) {
-    const int i = i0 + tid;
+  for (int i0 = 0; i0 < n_cand; i0 += NWA * 64) {
+    const int code = i0 + tid, i = pairs ? code % n_qb : code;
     bool sees = false;
-    if (i < n_qb) {
+    if (code < n_cand) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int qg = 2 * i + u;
         if (qg < n32) {
           const QueryHull h = hulls[qg];
-          sees |= h.lo < kbase + BK && h.hi > kbase;
+          bool on = h.lo < kbase + BK && h.hi > kbase;
+          if (BIAS && pairs && on) {
+            const uint8_t* live = a.live + ((int64_t)b * Hq + kvh * G + code / n_qb) * nblk;
+            on = false;
+            for (int k = max(kbase >> 5, h.lo >> 5); k < min((kbase + BK) >> 5, (h.hi + 31) >> 5); ++k)
+              on |= live[ds_block(qg, k, n32, causal)] != 0;
+          }
+          sees |= on;
         }
       }
     }
@@ -452,7 +481,7 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
       if (w < wave) at += counts[w];
       n_list += counts[w];
     }
-    if (sees) blocks[at + __popcll(bal & ((1ull << lane) - 1))] = (uint16_t)i;
+    if (sees) blocks[at + __popcll(bal & ((1ull << lane) - 1))] = (uint16_t)code;
     __syncthreads();
   }
   n_list = __builtin_amdgcn_readfirstlane(n_list);
@@ -479,11 +508,17 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
   // Within a head the blocks run last to first: the key tiles of one kv head
   // (on one XCD by the workgroup order) then move in step under a causal mask,
   // and share each Q / dO block through that XCD's L2.
-  const int total = G * n_list;
+  const int total = pairs ? n_list : G * n_list;
   const int it0 = (int)((int64_t)sp * total / nsh);
   const int n_iter = (int)((int64_t)(sp + 1) * total / nsh) - it0;
   auto pair_of = [&](int i, int& j, int& qbase) {   // j: query head within the group
     const int it = it0 + i;
+    if (BIAS && pairs) {                           // heads last to first too
+      const int code = __builtin_amdgcn_readfirstlane((int)blocks[n_list - 1 - it]);
+      j = code / n_qb;
+      qbase = code % n_qb * BQA;
+      return;
+    }
     j = it / n_list;
     qbase = __builtin_amdgcn_readfirstlane((int)blocks[n_list - 1 - it % n_list]) * BQA;
   };
@@ -576,7 +611,7 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
         };
         char* const dsb = reinterpret_cast<char*>(a.ds) +
                           (((int64_t)lbkv * G + j) * nblk + ds_block(qh >> 5, kw0 >> 5, n32, causal)) * kDsBlockBytes;
-        uint8_t* const live = a.live + ((int64_t)lbkv * G + j) * nblk + ds_block(qh >> 5, kw0 >> 5, n32, causal);
+        uint8_t* const live = a.live + ((int64_t)b * Hq + h) * nblk + ds_block(qh >> 5, kw0 >> 5, n32, causal);
         const bool full = kw0 >= all_lo && kw0 + 32 <= all_hi;     // wave-uniform
         half8 fd, fv;
         if constexpr (BIAS) {
@@ -604,8 +639,10 @@ attn_mod_dkdv_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
             }
           }
           const bool none = full && __builtin_amdgcn_ballot_w64(!(mx < -kNoneBwd)) == 0 && all_finite(sacc1);
-          if (lane == 0) *live = !none;
-          if (none) return;
+          if (none) {
+            if (lane == 0) *live = kZeroBlock;     // not 0: other shares of the tile list the pair by it
+            return;
+          }
           fd = rdo(0);
           fv = rdv(0);
           __builtin_amdgcn_s_setprio(1);
@@ -999,7 +1036,7 @@ attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
       if (q >= n32) continue;
       const QueryHull hu = hulls[q];
       const bool on = hu.lo < hu.hi && kg >= hu.lo >> 5 && kg < (hu.hi + 31) >> 5 &&
-                      a.live[((int64_t)lbkv * G + j) * nblk + ds_block(q, kg, n32, causal)];
+                      a.live[((int64_t)b * Hq + h) * nblk + ds_block(q, kg, n32, causal)] == kLiveBlock;
       any |= on;
       if (u == wave) mine = on;
     }
@@ -1102,7 +1139,7 @@ attn_mod_dq_kernel(const AttnModBwdArgs a, int bkv0, int nb) {
       row_interval(a.mod, causal, b, S, q, lo, hi);
 #pragma nounroll
       for (int k = kg0 * 32; k < min(kg_end * 32, S); ++k) {
-        if (MARKS && !a.live[((int64_t)lbkv * G + j) * nblk + ds_block(qg, k >> 5, n32, causal)]) continue;
+        if (MARKS && a.live[((int64_t)b * Hq + h) * nblk + ds_block(qg, k >> 5, n32, causal)] != kLiveBlock) continue;
         const char* el = dsq + (int64_t)(k >> 5) * kDsBlockBytes + ((k & 31) + 32 * (pos >> 4)) * 32 + (pos & 15) * 2;
         add_row(acc, (k >= lo) & (k < hi), (float)*reinterpret_cast<const _Float16*>(el),
                 Kp + (int64_t)k * a.kv_stride, g);

@@ -92,8 +92,8 @@ inline AttnModPlan attn_mod_plan(int B, int S, int Hq, int Hkv, int D, int causa
 // Workspace parts of the backward, in order, each 256-byte aligned: D and the
 // base-2 LSE [B, Hq, S] FP32, the rows' intervals [2][B, S] and the hulls
 // [B][ceil(S / 32)], a bit for every query of a head (tiles of kSharpTile), one chunk's
-// dS blocks and, with a distance bias, a byte for each of them, one chunk's
-// partial dK and dV.
+// dS blocks, a byte for every dS block of every head (used with a distance bias), one
+// chunk's partial dK and dV.
 constexpr int kSharpTile = 128;
 struct AttnModWs {
   size_t lse2, rows, hulls, sharp, ds, live, part, total;
@@ -107,9 +107,9 @@ inline AttnModWs attn_mod_ws(int B, int S, int Hq, int Hkv, int D, int causal) {
   w.hulls = w.rows + align256((size_t)2 * B * S * sizeof(int32_t));
   w.sharp = w.hulls + align256((size_t)B * n32 * sizeof(QueryHull));
   w.ds = w.sharp + align256((size_t)B * Hq * (((size_t)S + kSharpTile - 1) / kSharpTile) * (kSharpTile / 8));
-  const size_t blocks = (size_t)p.chunk * (Hq / Hkv) * (size_t)attn_bwd_ds_blocks(S, causal);
-  w.live = w.ds + align256(blocks * kDsBlockBytes);
-  w.part = w.live + align256(blocks);
+  const size_t blocks = (size_t)attn_bwd_ds_blocks(S, causal);
+  w.live = w.ds + align256((size_t)p.chunk * (Hq / Hkv) * blocks * kDsBlockBytes);
+  w.part = w.live + align256((size_t)B * Hq * blocks);
   w.total = w.part + (p.nsplit > 1 ? align256((size_t)2 * p.chunk * p.nsplit * S * D * sizeof(float)) : 0);
   return w;
 }
@@ -136,7 +136,7 @@ struct AttnModBwdArgs {
   QueryHull* hulls;
   uint32_t* sharp;
   lt_half* ds;
-  uint8_t* live;          // 0: the block is all zeros and was not written
+  uint8_t* live;          // [B, Hq] blocks: kLiveBlock, or the block is not written
   float* part;
 };
 

@@ -62,7 +62,7 @@ hipError_t attn_mod_bwd_launch(const AttnModBwdArgs& a, hipStream_t) {
   at = inside(a.sharp, (size_t)s.B * s.Hq * (((size_t)s.S + 127) / 128) * 16, at, "marks");
   const size_t blocks = s.causal ? n32 * (n32 + 1) / 2 : n32 * n32;
   at = inside(a.ds, (size_t)a.plan.chunk * grp * blocks * 2048, at, "dS blocks");
-  at = inside(a.live, (size_t)a.plan.chunk * grp * blocks, at, "dS marks");
+  at = inside(a.live, (size_t)s.B * s.Hq * blocks, at, "dS marks");
   if (a.plan.nsplit > 1) inside(a.part, (size_t)2 * a.plan.chunk * a.plan.nsplit * s.S * s.D * 4, at, "partials");
   return hipErrorNoDevice;
 }

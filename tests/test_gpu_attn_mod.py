@@ -390,3 +390,43 @@ def test_gradients_of_concentrated_softmax(env, kind, cap, std):
             e = np.linalg.norm(got[n][0, :, h].astype(np.float64) - r[m]) / np.linalg.norm(r[m])
             print(kind, h, n, e, flush=True)
             assert e <= math.sqrt(2 / 3) * H
+
+
+@pytest.mark.parametrize("B,S,Hq,Hkv,D,kind,slope,cap", [
+    (1, 1500, 2, 2, 128, "causal", 1.0, 0.0), (1, 1300, 4, 1, 64, "full", 0.5, 0.0), (2, 900, 4, 2, 128, "docs", 2.0, 20.0),
+    (1, 2100, 2, 1, 64, "prefix", 0.3, 0.0), (1, 1000, 8, 1, 128, "window", 4.0, 0.0), (1, 1200, 2, 2, 64, "wild", 0.7, 0.0)])
+def test_steep_bias(env, B, S, Hq, Hkv, D, kind, slope, cap):
+    """Slopes that leave most pairs without weight, next to flat heads: tiles that end after their scores."""
+    print("steep bias", B, S, Hq, Hkv, D, kind, slope, cap, flush=True)
+    rng, x = inputs(90 + S, B, S, Hq, Hkv, D)
+    mask = make_mask(kind, B, S, rng)
+    slopes = np.array([slope * (1.0 if h % 2 == 0 else 0.01) for h in range(Hq)], np.float32)
+    got = run_gpu(env, x, Hkv, D, 0.1, mask, cap, slopes)
+    check(got, x, Hkv, 0.1, mask, cap, slopes, {(B - 1, Hkv - 1)})
+    again = run_gpu(env, x, Hkv, D, 0.1, mask, cap, slopes)
+    for n in got:
+        assert np.array_equal(got[n].view(np.uint8), again[n].view(np.uint8)), n
+
+
+def test_bias_that_grows_with_distance(env):
+    """A negative slope: the farthest keys weigh most."""
+    rng, x = inputs(99, 1, 800, 2, 1, 64)
+    mask, slopes = make_mask("causal", 1, 800, rng), np.array([-0.5, 0.25], np.float32)
+    got = run_gpu(env, x, 1, 64, 0.125, mask, 0.0, slopes)
+    check(got, x, 1, 0.125, mask, 0.0, slopes)
+
+
+def test_chunks_of_heads(env):
+    """dS blocks of more than 8 GiB: the pairs of batch row and kv head go in chunks."""
+    torch, lt = env
+    B, S, Hq, Hkv, D = 33, 1024, 128, 16, 64
+    rng = np.random.Generator(np.random.PCG64(3))
+    mask = make_mask("docs_full", B, S, rng)
+    n32 = S // 32
+    assert lt.lt_attn_mod_bwd_workspace_size(B, S, Hq, Hkv, D, 0) < B * Hq * n32 * n32 * 2048   # chunks
+    g = torch.Generator()
+    g.manual_seed(5)
+    x = {n: torch.randn(B, S, h, D, generator=g).half().numpy() for n, h in
+         (("Q", Hq), ("K", Hkv), ("V", Hkv), ("dO", Hq))}
+    got = run_gpu(env, x, Hkv, D, 0.125, mask, 0.0, None)
+    check(got, x, Hkv, 0.125, mask, 0.0, None, {(0, 0), (16, 7), (16, 8), (32, 15)})

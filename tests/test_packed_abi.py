@@ -136,7 +136,7 @@ def test_workspace_sizes():
         blocks = n32 * (n32 + 1) // 2 if causal else n32 * n32
         return (2 * up(4 * B * Hq * S) + up(8 * B * S) + up(16 * B * n32) + up(16 * B * Hq * -(-S // 128)) +
                 up(chunk * (Hq // Hkv) * blocks * 2048) +
-                up(chunk * (Hq // Hkv) * blocks) +
+                up(B * Hq * blocks) +
                 (up(8 * chunk * nsplit * S * D) if nsplit > 1 else 0))
     # enough key tiles: one chunk, no shares; short sequences of few heads: shares, or not
     assert lt.lt_attn_mod_bwd_workspace_size(1, 4096, 32, 32, 128, 1) == attn(1, 4096, 32, 32, 128, 1, 32, 1)
