@@ -460,8 +460,8 @@ lt_status lt_rope_f16(lt_half* X, int64_t row_stride, int B, int S, int heads,
  *   slopes: [Hq] FP32 device array or NULL.  cap: 0 for none, else up to 1000.
  *   Layouts, head grouping and errors as lt_attn_fwd, and
  *   LT_ERR_INVALID_ARG for a cap that is negative or not finite;
- *   LT_ERR_UNSUPPORTED for cap > 1000, S > 2^19, or LO, HI, slopes not 4-byte
- *   aligned.
+ *   LT_ERR_UNSUPPORTED for cap > 1000, S > 2^19, B Hq ceil(S / 64) > 2^22, or
+ *   LO, HI, slopes not 4-byte aligned.
  */
 lt_status lt_attn_mod_fwd(const lt_half* Q, const lt_half* K, const lt_half* V,
                           int64_t q_row_stride, int64_t kv_row_stride,
@@ -510,8 +510,8 @@ lt_status lt_attn_mod_bwd(const lt_half* Q, const lt_half* K, const lt_half* V,
  *   the backward.  FP32 math, one rounding per output.
  *   Errors: LT_ERR_INVALID_ARG for NULL pointers, sizes < 1, strides below
  *   (Hq + Hkv) D, POS NULL with S > P, eps negative or not finite;
- *   LT_ERR_UNSUPPORTED for D not a multiple of 16 or above 256, misaligned
- *   pointers (16 bytes; POS, RSTD 4) or strides.
+ *   LT_ERR_UNSUPPORTED for D not a multiple of 16 or above 256, B S > 2^25,
+ *   misaligned pointers (16 bytes; POS, RSTD 4) or strides.
  */
 lt_status lt_qknorm_rope_fwd(const lt_half* X, int64_t ldx, const lt_half* Wq,
                              const lt_half* Wk, const float* CS, int P,

@@ -26,8 +26,11 @@ lt_status from_hip(hipError_t e, const char* what) {
 
 bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// the launches form element counts and workgroup counts from these products
+// element counts are formed from these products
 constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;
+// a launch has fewer than 2^32 threads: 64-query tiles of at most 512, tokens of 64
+constexpr int64_t kMaxTiles = (int64_t)1 << 22;
+constexpr int64_t kMaxTokens = (int64_t)1 << 25;
 
 // rows of up to 256 are loaded with 32-bit byte offsets
 constexpr int64_t kMaxAttnStride = (int64_t)1 << 22;
@@ -46,7 +49,7 @@ lt_status check_workspace(const void* ws, size_t given, size_t need) {
 
 bool attn_mod_shape_ok(int B, int S, int Hq, int Hkv, int D) {
   return B >= 1 && S >= 1 && Hq >= 1 && Hkv >= 1 && Hq % Hkv == 0 && (D == 64 || D == 128) && S <= lt::kModMaxS &&
-         !too_many((int64_t)B * S, Hq);
+         !too_many((int64_t)B * S, Hq) && ((int64_t)S + 63) / 64 * B * Hq <= kMaxTiles;
 }
 
 lt_status check_attn_mod(const void* Q, const void* K, const void* V, int64_t q_stride, int64_t kv_stride,
@@ -73,7 +76,7 @@ lt_status check_attn_mod(const void* Q, const void* K, const void* V, int64_t q_
     return fail(LT_ERR_UNSUPPORTED, "Q/K/V/O must be 16-byte aligned");
   if (!aligned(LSE, 4) || !aligned(m.lo, 4) || !aligned(m.hi, 4) || !aligned(m.slopes, 4))
     return fail(LT_ERR_UNSUPPORTED, "LSE, LO, HI and slopes must be 4-byte aligned");
-  if (too_many((int64_t)B * S, Hq)) return fail(LT_ERR_UNSUPPORTED, "B*S*Hq too large");
+  if (!attn_mod_shape_ok(B, S, Hq, Hkv, D)) return fail(LT_ERR_UNSUPPORTED, "B*S*Hq too large");
   return LT_OK;
 }
 
@@ -90,7 +93,8 @@ lt_status check_qknorm(const void* X, int64_t ldx, const void* Wq, const void* W
   if (!aligned(X, 16) || !aligned(Wq, 16) || !aligned(Wk, 16) || !aligned(CS, 16) || !aligned(Y, 16))
     return fail(LT_ERR_UNSUPPORTED, "X, weights, CS and outputs must be 16-byte aligned");
   if (!aligned(RSTD, 4) || !aligned(POS, 4)) return fail(LT_ERR_UNSUPPORTED, "RSTD and POS must be 4-byte aligned");
-  if (too_many((int64_t)B * S, (int64_t)Hq + Hkv)) return fail(LT_ERR_UNSUPPORTED, "B*S*(Hq+Hkv) too large");
+  if (too_many((int64_t)B * S, (int64_t)Hq + Hkv) || (int64_t)B * S > kMaxTokens)
+    return fail(LT_ERR_UNSUPPORTED, "B*S or B*S*(Hq+Hkv) too large");
   return LT_OK;
 }
 
@@ -193,7 +197,7 @@ lt_status lt_qknorm_rope_fwd(const lt_half* X, int64_t ldx, const lt_half* Wq, c
 
 size_t lt_qknorm_rope_bwd_workspace_size(int B, int S, int Hq, int Hkv, int D) {
   if (B < 1 || S < 1 || Hq < 1 || Hkv < 1 || D < 2 || (D & 15) || D > 256 ||
-      too_many((int64_t)B * S, (int64_t)Hq + Hkv))
+      too_many((int64_t)B * S, (int64_t)Hq + Hkv) || (int64_t)B * S > kMaxTokens)
     return 0;
   return lt::qknorm_bwd_ws_bytes((int64_t)B * S, D);
 }

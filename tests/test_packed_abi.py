@@ -49,6 +49,7 @@ FWD = dict(Q=FAKE, K=FAKE, V=FAKE, q_row_stride=384, kv_row_stride=384, O=FAKE, 
     (dict(D=96, o_row_stride=192), UNS), (dict(S=(1 << 19) + 1), UNS), (dict(q_row_stride=388), UNS), (dict(kv_row_stride=1 << 22), UNS),
     (dict(o_row_stride=1 << 22), UNS), (dict(K=FAKE + 8), UNS), (dict(O=FAKE + 2), UNS), (dict(LO=FAKE + 2), UNS),
     (dict(HI=FAKE + 1), UNS), (dict(slopes=FAKE + 2), UNS), (dict(B=1 << 27, S=1 << 19), UNS),
+    (dict(B=1 << 22, S=1), UNS),
 ])
 def test_attention_refusals(kw, st):
     assert status(lt.lt_attn_mod_fwd, FWD, **kw) == st
@@ -79,7 +80,7 @@ NORM = dict(X=FAKE, ldx=512, Wq=FAKE, Wk=FAKE, CS=FAKE, P=64, POS=None, RSTD=FAK
     (dict(X=None), INV), (dict(Wk=None), INV), (dict(CS=None), INV), (dict(RSTD=None), INV), (dict(B=0), INV),
     (dict(Hkv=0), INV), (dict(P=0), INV), (dict(S=65), INV), (dict(ldx=504), INV), (dict(D=120, ldx=480), UNS),
     (dict(D=272, ldx=1088), UNS), (dict(ldx=516), UNS), (dict(Wq=FAKE + 8), UNS), (dict(CS=FAKE + 4), UNS),
-    (dict(POS=FAKE + 2), UNS), (dict(RSTD=FAKE + 2), UNS), (dict(B=1 << 30, S=64), UNS),
+    (dict(POS=FAKE + 2), UNS), (dict(RSTD=FAKE + 2), UNS), (dict(B=1 << 30, S=64), UNS), (dict(B=1 << 20, S=33), UNS),
 ])
 def test_qknorm_refusals(kw, st):
     big = dict(ldy=2048) if kw.get("D", 0) > 128 else dict(ldy=512)
