@@ -266,7 +266,9 @@ attn_mod_delta_kernel(const AttnModBwdArgs a, int all, unsigned n_tile) {
     loaded_here(qf[kk]);
     loaded_here(gf[kk]);
   }
-  float dex = 0.f;                                 // this lane's share of D
+  // this lane's shares of sum P dP and of sum P, which the LSE's rounding leaves 1e-7 or
+  // so off 1: their quotient is a D that a row of one key cancels exactly
+  float dex = 0.f, psum = 0.f;
   auto slice = [&](int kt, auto CUR_) {
     constexpr int cur = decltype(CUR_)::value;
     const char* st = smem + cur * STAGE;
@@ -340,20 +342,25 @@ attn_mod_delta_kernel(const AttnModBwdArgs a, int all, unsigned n_tile) {
 #pragma unroll
         for (int kb = 0; kb < KBW; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[kb][r] = fast_exp2(fmaf(sacc[kb][r], sc.c, -lse2)) * pacc[kb][r];
+          for (int r = 0; r < 16; ++r) sacc[kb][r] = fast_exp2(fmaf(sacc[kb][r], sc.c, -lse2));
         if (!full) {
 #pragma unroll
           for (int kb = 0; kb < KBW; ++kb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
               const int key = key0 + kb * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-              sacc[kb][r] = ((key >= lo) & (key < hi)) ? sacc[kb][r] : 0.f;
+              const bool see = (key >= lo) & (key < hi);
+              sacc[kb][r] = see ? sacc[kb][r] : 0.f;
+              pacc[kb][r] = see ? pacc[kb][r] : 0.f;
             }
         }
 #pragma unroll
         for (int kb = 0; kb < KBW; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) dex += sacc[kb][r];
+          for (int r = 0; r < 16; ++r) {
+            psum += sacc[kb][r];
+            dex = fmaf(sacc[kb][r], pacc[kb][r], dex);
+          }
       }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -364,14 +371,17 @@ attn_mod_delta_kernel(const AttnModBwdArgs a, int all, unsigned n_tile) {
     if (kt + 1 < kt1) slice(kt + 1, std::integral_constant<int, 1>{});
   }
   dex += __shfl_xor(dex, 32);
+  psum += __shfl_xor(psum, 32);
   if constexpr (QSPLIT > 1) {
-    float* red = reinterpret_cast<float*>(smem);   // free after the loop's last barrier
-    if (kpart == 1) red[qg * 64 + lane] = dex;
+    float2* red = reinterpret_cast<float2*>(smem); // free after the loop's last barrier
+    if (kpart == 1) red[qg * 64 + lane] = make_float2(dex, psum);
     __syncthreads();
     if (kpart == 1) return;
-    dex += red[qg * 64 + lane];
+    const float2 o = red[qg * 64 + lane];
+    dex += o.x;
+    psum += o.y;
   }
-  if (myq < S && g == 0 && lo < hi && sharp != 0) a.delta[ri] = dex;
+  if (myq < S && g == 0 && lo < hi && sharp != 0) a.delta[ri] = dex / psum;
 }
 
 // ------------------------------------------------------------ 2: dK/dV

@@ -392,6 +392,28 @@ def test_gradients_of_concentrated_softmax(env, kind, cap, std):
             assert e <= math.sqrt(2 / 3) * H
 
 
+@pytest.mark.parametrize("S,D,cap", [(1, 64, 0.0), (40, 128, 0.0), (400, 64, 30.0), (600, 128, 0.0)])
+def test_rows_of_one_key_have_no_gradient(env, S, D, cap):
+    """Every query sees itself alone: P = 1 and D = dP, so dQ = dK = 0, however large the score.  V and dO are
+    small integers, so that dP is exact in any order; then D = (p dP) / p is off by two roundings,
+    |dP - D| <= 2^-23 |dP|, P by less than 2^-10, and dS gains half an FP16 step or subnormal step.  A D that
+    took sum P for 1 would be off by the rounding of the LSE, 2^-20 for the largest scores here."""
+    rng, x = inputs(70 + S, 1, S, 2, 1, D, 6.0)
+    for n in ("V", "dO"):
+        x[n] = rng.integers(-8, 9, size=x[n].shape).astype(np.float16)
+    i = np.arange(S, dtype=np.int32)[None]
+    scale = 1 / math.sqrt(D)
+    got = run_gpu(env, x, 1, D, scale, (i, None, 1), cap, None)
+    dk = np.zeros((S, D))
+    for h in range(2):
+        q, k, v, do = (x[n][0, :, m].astype(np.float64) for n, m in (("Q", h), ("K", 0), ("V", 0), ("dO", h)))
+        ds = (2.0 ** -23 * np.abs((do * v).sum(1)) * (1 + 2.0 ** -10) * (1 + H) + SUB)[:, None] * scale
+        assert np.array_equal(got["O"][0, :, h], x["V"][0, :, 0])
+        assert np.all(np.abs(got["dQ"][0, :, h]) <= ds * np.abs(k) * (1 + 2 * H) + SUB)
+        dk += ds * np.abs(q)
+    assert np.all(np.abs(got["dK"][0, :, 0]) <= dk * (1 + 2 * H) + SUB)
+
+
 @pytest.mark.parametrize("B,S,Hq,Hkv,D,kind,slope,cap", [
     (1, 1500, 2, 2, 128, "causal", 1.0, 0.0), (1, 1300, 4, 1, 64, "full", 0.5, 0.0), (2, 900, 4, 2, 128, "docs", 2.0, 20.0),
     (1, 2100, 2, 1, 64, "prefix", 0.3, 0.0), (1, 1000, 8, 1, 128, "window", 4.0, 0.0), (1, 1200, 2, 2, 64, "wild", 0.7, 0.0)])
