@@ -232,51 +232,66 @@ embed_walk_kernel(const EmbedBwdArgs a, int parts, int ncb) {
 }
 
 // ------------------------------------------------------------ 3: join
-// (kEmbedPart positions, 512 columns): the long run that starts there, if there is one
-// (it holds the last of them).  Each wave adds a quarter of its partial rows, then
-// the first the quarters, in order.
+// Workgroup = (kJoinSpan windows of kEmbedPart positions, 256 columns), for the long runs
+// that start there (a window holds the start of one at most, and its last token is of
+// that run).  Each of 8 thread groups adds an eighth of the partial rows, eight loads
+// in flight, then the groups' sums are added, all in order.  Bound by latency and by the
+// longest run, hence the narrow columns: the gradient of 16384 tokens of 32000 x 4096 takes
+// 78 us, with half of the tokens the same 100, all 131 (one group of four waves per 512 columns:
+// 107 and 156); a window a workgroup costs ordinary texts 3 us, four 4.
+constexpr int kJoinSpan = 2;
+constexpr int kJoinLanes = 32, kJoinGroups = kThreads / kJoinLanes;
 __global__ void __launch_bounds__(kThreads)
 embed_join_kernel(const EmbedBwdArgs a) {
-  __shared__ float red[kRowWaves - 1][64 * 8];
   constexpr int C = kEmbedPart;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ float red[kJoinGroups][kJoinLanes * 8];
+  const int lane = threadIdx.x & 63, grp = threadIdx.x / kJoinLanes, c = threadIdx.x % kJoinLanes;
   const int n = a.start[a.V];
-  const int p0 = blockIdx.x * C, p1 = min(p0 + C, n);
-  if (p0 >= p1) return;
-  const int64_t v = a.ids[a.tokens[p1 - 1]];
-  const int s = a.start[v], e = a.start[v + 1];
-  if (e - s <= C || s < p0) return;                  // uniform
-  const int64_t col = ((int64_t)blockIdx.y * 64 + lane) * 8;
+  // lane = window
+  int v = 0, s = 0, e = 0;
+  bool mine = false;
+  const int p0 = ((int)blockIdx.x * kJoinSpan + lane) * C;
+  if (lane < kJoinSpan && p0 < n) {
+    v = (int)a.ids[a.tokens[min(p0 + C, n) - 1]];
+    s = a.start[v];
+    e = a.start[v + 1];
+    mine = e - s > C && s >= p0;
+  }
+  uint64_t runs = __builtin_amdgcn_ballot_w64(mine);           // the same in every wave
+  const int64_t col = ((int64_t)blockIdx.y * kJoinLanes + c) * 8;
   const bool in = col < a.H;
-  const int pieces = (e - s + C - 1) / C, per = (pieces + kRowWaves - 1) / kRowWaves;
-  const int k0 = wave * per, k1 = min(k0 + per, pieces);
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int k = k0; k < k1; k += 4) {
-    float4 x[4], y[4];
+  for (; runs != 0; runs &= runs - 1) {
+    const int w = __builtin_ctzll(runs);
+    const int sw = __builtin_amdgcn_readlane(s, w), ew = __builtin_amdgcn_readlane(e, w);
+    const int pieces = (ew - sw + C - 1) / C, per = (pieces + kJoinGroups - 1) / kJoinGroups;
+    const int k0 = grp * per, k1 = min(k0 + per, pieces);
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int k = k0; k < k1; k += 8) {
+      float4 x[8], y[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const float* src = a.part + part_row(s + (k + u) * C, k + u) * a.H + col;
-      const bool ok = in && k + u < k1;
-      x[u] = ok ? *reinterpret_cast<const float4*>(src) : make_float4(0.f, 0.f, 0.f, 0.f);
-      y[u] = ok ? *reinterpret_cast<const float4*>(src + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int u = 0; u < 8; ++u) {
+        const float* src = a.part + part_row(sw + (k + u) * C, k + u) * a.H + col;
+        const bool ok = in && k + u < k1;
+        x[u] = ok ? *reinterpret_cast<const float4*>(src) : make_float4(0.f, 0.f, 0.f, 0.f);
+        y[u] = ok ? *reinterpret_cast<const float4*>(src + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        acc[0] += x[u].x; acc[1] += x[u].y; acc[2] += x[u].z; acc[3] += x[u].w;
+        acc[4] += y[u].x; acc[5] += y[u].y; acc[6] += y[u].z; acc[7] += y[u].w;
+      }
     }
+    __syncthreads();                                 // red is free
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      acc[0] += x[u].x; acc[1] += x[u].y; acc[2] += x[u].z; acc[3] += x[u].w;
-      acc[4] += y[u].x; acc[5] += y[u].y; acc[6] += y[u].z; acc[7] += y[u].w;
+    for (int q = 0; q < 8; ++q) red[grp][c * 8 + q] = acc[q];
+    __syncthreads();
+    if (grp == 0 && in) {
+      for (int r = 1; r < kJoinGroups; ++r)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) acc[q] += red[r][c * 8 + q];
+      store_row(a, __builtin_amdgcn_readlane(v, w), col, acc);
     }
   }
-  if (wave > 0) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) red[wave - 1][lane * 8 + q] = acc[q];
-  }
-  __syncthreads();
-  if (wave > 0 || !in) return;
-#pragma unroll
-  for (int w = 0; w < kRowWaves - 1; ++w)
-#pragma unroll
-    for (int q = 0; q < 8; ++q) acc[q] += red[w][lane * 8 + q];
-  store_row(a, v, col, acc);
 }
 
 // ------------------------------------------------------------ few tokens: scan
@@ -350,7 +365,9 @@ hipError_t embed_bwd_launch(const EmbedBwdArgs& a, hipStream_t s) {
   const int64_t rows = a.accumulate ? 0 : (a.V + kRowWaves - 1) / kRowWaves;
   hipLaunchKernelGGL(embed_walk_kernel, dim3((unsigned)(parts * wide + rows)), dim3(kThreads), 0, s, a, parts, wide);
   if ((e = hipGetLastError()) != hipSuccess || a.T <= kEmbedPart) return e;
-  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)parts, (unsigned)((a.H + 511) / 512)), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(embed_join_kernel,
+                     dim3((unsigned)((parts + kJoinSpan - 1) / kJoinSpan),
+                     (unsigned)((a.H / 8 + kJoinLanes - 1) / kJoinLanes)), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
