@@ -509,7 +509,8 @@ lt_status lt_attn_mod_bwd(const lt_half* Q, const lt_half* K, const lt_half* V,
  *   (ldy = ldx) where no backward follows.  RSTD [T, Hq + Hkv] FP32: r, kept for
  *   the backward.  FP32 math, one rounding per output.
  *   Errors: LT_ERR_INVALID_ARG for NULL pointers, sizes < 1, strides below
- *   (Hq + Hkv) D, POS NULL with S > P, eps negative or not finite;
+ *   (Hq + Hkv) D, in place with two strides, POS NULL with S > P, eps negative
+ *   or not finite;
  *   LT_ERR_UNSUPPORTED for D not a multiple of 16 or above 256, B S > 2^25,
  *   misaligned pointers (16 bytes; POS, RSTD 4) or strides.
  */

@@ -11,15 +11,25 @@
 //     block of each slice each and merge their states through LDS;
 //   * S^T = K Q^T with 32x32x16 MFMA, so that a lane owns one query and its
 //     interval sits in two registers.  The workgroup walks the 64-key slices of
-//     the hull of its queries' intervals, a wave skips the slices that none of
-//     its 32 queries sees and compares key against interval only in slices that
-//     some of them see in part;
+//     the hull of its queries' intervals, last slice first (under a causal mask the
+//     nearest keys, which a distance bias makes the heaviest), a wave skips the slices
+//     that none of its 32 queries sees, compares key against interval only in
+//     slices that some of them see in part, and with a distance bias leaves a slice
+//     after its scores where none has weight;
 //   * K and V slices go HBM -> LDS by direct loads, double-buffered; O^T += V^T P^T
 //     takes V^T by the LDS transpose read in the accumulator's key order, so that
 //     P goes from the score registers, rounded to FP16 (the rounding of every
 //     FP16 matrix operand), straight into the product;
 //   * one pass: running maximum and sum in FP32, the maximum raised only when a
 //     row exceeds it by more than 2^8 in probability.
+//
+// Bound by the matrix and vector units in turn: two waves a SIMD, whose products and
+// softmax overlap poorly.  4 D flop a visible pair: 8192 tokens of 64:8 heads in six
+// documents 528 us (827 TFLOP/s; a large matrix product reaches 1300 here), 4096 tokens of 32
+// heads causal 156 us (880), with a cap 199 (690: an exp2 and a reciprocal more a score),
+// 40 heads with ALiBi slopes 157 (steep heads leave most slices after their scores).
+// One wave a SIMD with the next slice's scores placed under this one's softmax needs more
+// registers than there are: 396 spilled, 567 TFLOP/s.
 
 #include <type_traits>
 

@@ -31,7 +31,8 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// tpr threads per token row (a power of two), kThreads / tpr rows per workgroup
+// tpr threads per token row (a power of two), kThreads / tpr rows per workgroup.  4096 rows
+// of 4096 10 us (6.9 TB/s; the rows partly from cache), 8191 rows of 5120 25 us (6.6).
 __global__ void __launch_bounds__(kThreads)
 embed_fwd_kernel(const int64_t* __restrict__ ids, const lt_half* __restrict__ W, int64_t ldw, float scale,
                  lt_half* __restrict__ Y, int64_t ldy, int64_t T, int nch, int64_t V, int tpr) {
@@ -53,7 +54,8 @@ constexpr int kSortWaves = 16;
 constexpr int kSortMaxRows = 1024;
 constexpr int kIdBatches = 8;          // 64-id batches a wave loads together
 
-// range: rows v0 .. v0 + R - 1, R = 1 << bits
+// range: rows v0 .. v0 + R - 1, R = 1 << bits.  Latency-bound: two passes over the ids,
+// 4096 of them in 7 us, 8191 in 12.5.
 __global__ void __launch_bounds__(64 * kSortWaves)
 embed_sort_kernel(const int64_t* __restrict__ ids, int64_t T, int64_t V, int bits, int32_t* __restrict__ start,
                   int32_t* __restrict__ tokens) {
@@ -165,6 +167,8 @@ __device__ __forceinline__ int64_t part_row(int p, int k) { return 2 * (int64_t)
 // runs, and the pieces of long runs, that start in their positions: at most
 // 2 kEmbedPart - 1 tokens.  The others: a wave per row, zeros where no token falls
 // (non-temporal, so that they do not evict the tokens' rows; more rows a wave: level).
+// Bound by the writes of dW: 32000 x 4096 (262 MB) and 4096 tokens in 42 us, 152064 x 5120
+// (1557 MB) and 8191 tokens in 281 us (5.8 TB/s).
 __global__ void __launch_bounds__(kThreads)
 embed_walk_kernel(const EmbedBwdArgs a, int parts, int ncb) {
   constexpr int C = kEmbedPart;

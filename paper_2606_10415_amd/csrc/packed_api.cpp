@@ -95,6 +95,7 @@ lt_status check_qknorm(const void* X, int64_t ldx, const void* Wq, const void* W
   if (!aligned(RSTD, 4) || !aligned(POS, 4)) return fail(LT_ERR_UNSUPPORTED, "RSTD and POS must be 4-byte aligned");
   if (too_many((int64_t)B * S, (int64_t)Hq + Hkv) || (int64_t)B * S > kMaxTokens)
     return fail(LT_ERR_UNSUPPORTED, "B*S or B*S*(Hq+Hkv) too large");
+  if (X == Y && ldx != ldy) return fail(LT_ERR_INVALID_ARG, "in place: one row stride");
   return LT_OK;
 }
 
@@ -213,6 +214,7 @@ lt_status lt_qknorm_rope_bwd(const lt_half* dY, int64_t lddy, const lt_half* X, 
   if (lddy & 7) return fail(LT_ERR_UNSUPPORTED, "row strides must be multiples of 8 elements");
   if (!aligned(dY, 16) || !aligned(dWq, 2) || !aligned(dWk, 2))
     return fail(LT_ERR_UNSUPPORTED, "dY must be 16-byte, dWq and dWk 2-byte aligned");
+  if (dY == dX && lddy != lddx) return fail(LT_ERR_INVALID_ARG, "in place: one row stride");
   if ((st = check_workspace(workspace, ws_bytes, lt::qknorm_bwd_ws_bytes((int64_t)B * S, D))) != LT_OK) return st;
   lt::QkNormArgs a{X, ldx, Wq, Wk, CS, P, POS, (int64_t)B * S, S, Hq, Hkv, D};
   return from_hip(lt::qknorm_bwd_launch(a, dY, lddy, RSTD, dX, lddx, dWq, dWk, static_cast<float*>(workspace),

@@ -44,8 +44,8 @@ class DecoderLayer:
     ``shape`` needs attributes B, S, H, Hq, Hkv, D, F.  ``params`` maps
     X, dY, Wqkv, Wo, Wgu, Wd to float16 tensors (host or device).  ``norm``
     (optional) has attributes wn1, wn2 (RMSNorm weights [H]), eps, rope_base (or
-    None) and optionally bqkv (QKV projection bias), wq and wk (head norm weights
-    [D]), each may be None.  ``attention`` (optional) is a packing.Attention.
+    None) and optionally bqkv (QKV projection bias, or None), wq and wk (head norm
+    weights [D], both or neither).  ``attention`` (optional) is a packing.Attention.
     ``fuse_swiglu`` selects the GEMMs with the SwiGLU epilogues.
     """
 
@@ -73,9 +73,13 @@ class DecoderLayer:
         self.Wd = dev(params["Wd"])
 
         self.rope = norm is not None and norm.rope_base is not None
-        self.qk_norm = norm is not None and getattr(norm, "wq", None) is not None
-        if self.qk_norm and not self.rope:
-            raise ValueError("QK norm comes with the rotary embedding: rope_base must be given")
+        wqk = [getattr(norm, n, None) for n in ("wq", "wk")]
+        self.qk_norm = wqk[0] is not None or wqk[1] is not None
+        if self.qk_norm:
+            if not self.rope:
+                raise ValueError("QK norm comes with the rotary embedding: rope_base must be given")
+            if any(w is None or tuple(w.shape) != (sh.D,) for w in wqk):
+                raise ValueError(f"QK norm takes weights [{sh.D}] for the query and for the key heads")
         self.attn = attention
         pos = None
         if attention is not None:
@@ -98,8 +102,11 @@ class DecoderLayer:
         # forward activations the backward reads (shareable between layers
         # whose forward is recomputed right before their backward)
         if share_acts is not None:
-            for k in ("QKV", "QKr", "O", "LSE", "H1", "GU", "A"):
+            for k in ("QKV", "O", "LSE", "H1", "GU", "A"):
                 setattr(self, k, getattr(share_acts, k))
+            self.QKr = share_acts.QKr if self.qk_norm else self.QKV
+            if self.qk_norm and not share_acts.qk_norm:
+                raise ValueError("a layer with QK norm shares the activations of another such layer")
         else:
             self.QKV = e(T, self.qkv)
             # rotated Q and K, rows as far apart as QKV's (attention takes K and V with one row stride)

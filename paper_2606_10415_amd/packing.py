@@ -17,7 +17,8 @@ class Attention:
 
     lo, hi: int32 [B, S] or None; causal: only keys up to the query; cap: tanh cap of the
     scores, 0 for none; slopes: distance bias per query head, or None; pos: int32 [B, S]
-    positions for the rotary embedding (used with QK norm), None for 0 .. S - 1 per row.
+    positions for the rotary embedding with QK norm, None for 0 .. S - 1 per row.  The rotation
+    without QK norm is by 0 .. S - 1: scores depend on the distance of two positions only.
     """
     lo: object = None
     hi: object = None

@@ -7,6 +7,7 @@ Frobenius error 5e-3 for one layer, 1e-2 for a stage of several.
 """
 
 import math
+from dataclasses import replace
 
 import numpy as np
 import pytest
@@ -185,8 +186,28 @@ def test_stage_refusals(torch):
         DecoderLayer(W, p, attention=packing.Attention(slopes=packing.alibi_slopes(5)))
     with pytest.raises(ValueError):
         DecoderLayer(W, p, norm=norms(W, 1, True, None))                              # QK norm without a rotary base
+    n = norms(W, 1)
+    for bad in (replace(n, wk=None), replace(n, wq=None), replace(n, wk=n.wk[:-8])):
+        with pytest.raises(ValueError):
+            DecoderLayer(W, p, norm=bad)
     with pytest.raises(ValueError):
         Stage(W, 1, embed=np.zeros((10, 128), np.float16))
+
+
+def test_shared_activations_of_layers_with_and_without_qk_norm(torch):
+    """A layer without QK norm that shares the activations of one with it rotates Q and K in QKV."""
+    from paper_2606_10415_amd.layer import DecoderLayer
+    p = layer_inputs(W)
+    plain, qk = norms(W, 5, False), norms(W, 5)
+    with pytest.raises(ValueError):
+        DecoderLayer(W, p, norm=qk, share_acts=DecoderLayer(W, p, norm=plain))
+    res = []
+    for share in (None, DecoderLayer(W, p, norm=qk)):
+        l = DecoderLayer(W, p, norm=plain, share_acts=share)
+        l.forward()
+        l.backward()
+        res.append((l.Y.cpu(), l.dX.cpu(), l.dWqkv.cpu()))
+    assert all(torch.equal(a, b) for a, b in zip(*res))
 
 
 def test_step_graph_replays_match_eager(torch):

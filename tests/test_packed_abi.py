@@ -93,11 +93,11 @@ def test_qknorm_refusals(kw, st):
 def test_qknorm_further_refusals():
     f = dict(NORM, Y=FAKE, ldy=512, eps=1e-6)
     for kw, st in ((dict(eps=-1.0), INV), (dict(eps=float("nan")), INV), (dict(Y=None), INV), (dict(ldy=8), INV),
-                   (dict(Y=FAKE + 8), UNS)):
+                   (dict(Y=FAKE + 8), UNS), (dict(ldy=520), INV)):
         assert status(lt.lt_qknorm_rope_fwd, f, **kw) == st
     n = lt.lt_qknorm_rope_bwd_workspace_size(2, 32, 3, 1, 128)
     b = dict(NORM, dY=FAKE, lddy=512, dX=FAKE, lddx=512, dWq=FAKE, dWk=FAKE, workspace=FAKE, ws_bytes=n)
-    for kw, st in ((dict(dY=None), INV), (dict(dWq=None), INV), (dict(lddy=8), INV), (dict(lddy=516), UNS),
+    for kw, st in ((dict(dY=None), INV), (dict(dWq=None), INV), (dict(lddy=8), INV), (dict(lddy=516), UNS), (dict(lddy=520), INV),
                    (dict(dWk=FAKE + 1), UNS), (dict(workspace=None), WS), (dict(ws_bytes=n - 1), WS)):
         assert status(lt.lt_qknorm_rope_bwd, b, **kw) == st
 
