@@ -165,19 +165,19 @@ __device__ __forceinline__ int64_t part_row(int p, int k) { return 2 * (int64_t)
 
 // Workgroups 0 .. parts x ncb - 1: (kEmbedPart positions, 2048 columns).  They take the
 // runs, and the pieces of long runs, that start in their positions: at most
-// 2 kEmbedPart - 1 tokens.  The others: a wave per row, zeros where no token falls
-// (non-temporal, so that they do not evict the tokens' rows; more rows a wave: level).
+// 2 kEmbedPart - 1 tokens.  The others: 2^zbits lanes a row (up to a wave), zeros where no token
+// falls (non-temporal, so that they do not evict the tokens' rows; more rows a wave: level).
 // Bound by the writes of dW: 32000 x 4096 (262 MB) and 4096 tokens in 42 us, 152064 x 5120
 // (1557 MB) and 8191 tokens in 281 us (5.8 TB/s).
 __global__ void __launch_bounds__(kThreads)
-embed_walk_kernel(const EmbedBwdArgs a, int parts, int ncb) {
+embed_walk_kernel(const EmbedBwdArgs a, int parts, int ncb, int zbits) {
   constexpr int C = kEmbedPart;
   static_assert(2 * C <= 64, "a lane per token");
   const int lane = threadIdx.x & 63;
   if (blockIdx.x >= (unsigned)(parts * ncb)) {
-    const int64_t v = (int64_t)(blockIdx.x - parts * ncb) * kRowWaves + (threadIdx.x >> 6);
+    const int64_t v = (int64_t)(blockIdx.x - parts * ncb) * (kThreads >> zbits) + (threadIdx.x >> zbits);
     if (v >= a.V || a.start[v] != a.start[v + 1]) return;
-    for (int64_t col = lane * 8; col < a.H; col += 64 * 8)
+    for (int64_t col = (threadIdx.x & ((1 << zbits) - 1)) * 8; col < a.H; col += 8 << zbits)
       __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4*>(a.dW + v * a.lddw + col));
     return;
   }
@@ -366,8 +366,11 @@ hipError_t embed_bwd_launch(const EmbedBwdArgs& a, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int parts = (int)embed_parts(a.T);
-  const int64_t rows = a.accumulate ? 0 : (a.V + kRowWaves - 1) / kRowWaves;
-  hipLaunchKernelGGL(embed_walk_kernel, dim3((unsigned)(parts * wide + rows)), dim3(kThreads), 0, s, a, parts, wide);
+  int zbits = 0;
+  while (zbits < 6 && (8 << zbits) < a.H) ++zbits;
+  const int64_t per = kThreads >> zbits, rows = a.accumulate ? 0 : (a.V + per - 1) / per;
+  hipLaunchKernelGGL(embed_walk_kernel, dim3((unsigned)(parts * wide + rows)), dim3(kThreads), 0, s, a, parts, wide,
+                     zbits);
   if ((e = hipGetLastError()) != hipSuccess || a.T <= kEmbedPart) return e;
   hipLaunchKernelGGL(embed_join_kernel,
                      dim3((unsigned)((parts + kJoinSpan - 1) / kJoinSpan),

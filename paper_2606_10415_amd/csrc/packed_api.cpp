@@ -200,7 +200,7 @@ size_t lt_qknorm_rope_bwd_workspace_size(int B, int S, int Hq, int Hkv, int D) {
   if (B < 1 || S < 1 || Hq < 1 || Hkv < 1 || D < 2 || (D & 15) || D > 256 ||
       too_many((int64_t)B * S, (int64_t)Hq + Hkv) || (int64_t)B * S > kMaxTokens)
     return 0;
-  return lt::qknorm_bwd_ws_bytes((int64_t)B * S, D);
+  return lt::qknorm_bwd_ws_bytes((int64_t)B * S, Hq, Hkv, D);
 }
 
 lt_status lt_qknorm_rope_bwd(const lt_half* dY, int64_t lddy, const lt_half* X, int64_t ldx, const lt_half* Wq,
@@ -215,7 +215,7 @@ lt_status lt_qknorm_rope_bwd(const lt_half* dY, int64_t lddy, const lt_half* X, 
   if (!aligned(dY, 16) || !aligned(dWq, 2) || !aligned(dWk, 2))
     return fail(LT_ERR_UNSUPPORTED, "dY must be 16-byte, dWq and dWk 2-byte aligned");
   if (dY == dX && lddy != lddx) return fail(LT_ERR_INVALID_ARG, "in place: one row stride");
-  if ((st = check_workspace(workspace, ws_bytes, lt::qknorm_bwd_ws_bytes((int64_t)B * S, D))) != LT_OK) return st;
+  if ((st = check_workspace(workspace, ws_bytes, lt::qknorm_bwd_ws_bytes((int64_t)B * S, Hq, Hkv, D))) != LT_OK) return st;
   lt::QkNormArgs a{X, ldx, Wq, Wk, CS, P, POS, (int64_t)B * S, S, Hq, Hkv, D};
   return from_hip(lt::qknorm_bwd_launch(a, dY, lddy, RSTD, dX, lddx, dWq, dWk, static_cast<float*>(workspace),
                                         reinterpret_cast<hipStream_t>(stream)),

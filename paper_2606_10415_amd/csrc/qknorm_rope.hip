@@ -9,9 +9,10 @@
 // HBM-bound: 4 bytes an element forth, 6 back.  Separate norm and rotation
 // passes would move 8 and 12.
 //   * one wave per token, so that the token's cosines and sines are read once
-//     for all its heads; D / 16 lanes (rounded up to a power of two) take a head,
-//     each with eight features and their rotation partners, so the rotation stays
-//     within a lane and the norm's sum is a few lane exchanges;
+//     for all its heads (few heads: several tokens, few tokens: several waves per token);
+//     D / 16 lanes (rounded up to a power of two) take a head, each with eight
+//     features and their rotation partners, so the rotation stays within a lane
+//     and the norm's sum is a few lane exchanges;
 //   * FP32 arithmetic, one rounding per output; r kept in FP32 for the backward;
 //   * backward: every lane keeps its FP32 part of dw for the query heads, then for
 //     the key heads (both at once take 200 registers and lose: 29 us for 27); a
@@ -55,18 +56,21 @@ __device__ __forceinline__ float row_sum(float v) {   // over the LPR lanes of a
 // LPR lanes per head row
 template <int LPR>
 __global__ void __launch_bounds__(64 * kWaves)
-qknorm_fwd_kernel(const QkNormArgs a, lt_half* Y, int64_t ldy, float* __restrict__ RSTD, float eps) {
+qknorm_fwd_kernel(const QkNormArgs a, const HeadSplit hs, lt_half* Y, int64_t ldy, float* __restrict__ RSTD,
+                  float eps) {
   constexpr int RPW = 64 / LPR;                    // head rows per wave
   const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (t >= a.T) return;                            // whole wave leaves together
-  const int i = lane % LPR;
+  const unsigned unit = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int row = lane / LPR, i = lane % LPR;
+  const int64_t t = (int64_t)(unit / hs.parts) * (RPW >> hs.shift) + (row >> hs.shift);
+  if (t >= a.T) return;                            // a head row's lanes leave together
   const int half = a.D / 2, heads = a.Hq + a.Hkv;
   const bool in = i * 8 < half;
   float co[8], si[8];
   load_angles(a, t, in ? i : 0, co, si);
   const float inv_d = 1.f / (float)a.D;
-  for (int h = lane / LPR; h < heads; h += RPW) {
+  const int first = ((unit % hs.parts) << hs.shift) + (row & ((1 << hs.shift) - 1));
+  for (int h = first; h < heads; h += hs.parts << hs.shift) {
     const lt_half* x = a.X + t * a.ldx + (int64_t)h * a.D + i * 8;
     const lt_half* w = (h < a.Hq ? a.Wq : a.Wk) + i * 8;
     const u32x4 zero = {0, 0, 0, 0};
@@ -95,29 +99,35 @@ qknorm_fwd_kernel(const QkNormArgs a, lt_half* Y, int64_t ldy, float* __restrict
 
 template <int LPR>
 __global__ void __launch_bounds__(64 * kWaves)
-qknorm_bwd_kernel(const QkNormArgs a, const lt_half* dY, int64_t lddy, const float* __restrict__ RSTD, lt_half* dX,
+qknorm_bwd_kernel(const QkNormArgs a, const HeadSplit hq, const HeadSplit hk, const lt_half* dY, int64_t lddy, const float* __restrict__ RSTD, lt_half* dX,
                   int64_t lddx, float* __restrict__ part) {
   constexpr int RPW = 64 / LPR;
   __shared__ float red[kWaves][LPR * 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int i = lane % LPR;
+  const int row = lane / LPR, i = lane % LPR;
   const int half = a.D / 2, heads = a.Hq + a.Hkv;
   const bool in = i * 8 < half;
   const float inv_d = 1.f / (float)a.D;
   const u32x4 zero = {0, 0, 0, 0};
-  // query heads, then key heads
+  // query heads, then key heads; with gridDim.y = 2 one of them
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
+    if (gridDim.y == 2 && (int)blockIdx.y != which) continue;
+    const HeadSplit hs = which ? hk : hq;
+    const unsigned units = (unsigned)hs.groups * hs.parts;
     const lt_half* W = which ? a.Wk : a.Wq;
     const int h0 = which ? a.Hq : 0, h1 = which ? heads : a.Hq;
     const half8 w1 = as_half8(in ? ld16(W + i * 8) : zero), w2 = as_half8(in ? ld16(W + half + i * 8) : zero);
     float dw[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) dw[e] = 0.f;
-    for (int64_t t = (int64_t)blockIdx.x * kWaves + wave; t < a.T; t += (int64_t)gridDim.x * kWaves) {
+    for (unsigned unit = blockIdx.x * kWaves + wave; unit < units; unit += gridDim.x * kWaves) {
+      const int64_t t = (int64_t)(unit / hs.parts) * (RPW >> hs.shift) + (row >> hs.shift);
+      if (t >= a.T) continue;                      // a head row's lanes together
       float co[8], si[8];
       load_angles(a, t, in ? i : 0, co, si);
-      for (int h = h0 + lane / LPR; h < h1; h += RPW) {
+      const int first = h0 + ((unit % hs.parts) << hs.shift) + (row & ((1 << hs.shift) - 1));
+      for (int h = first; h < h1; h += hs.parts << hs.shift) {
         const lt_half* x = a.X + t * a.ldx + (int64_t)h * a.D + i * 8;
         const lt_half* dy = dY + t * lddy + (int64_t)h * a.D + i * 8;
         const half8 x1 = as_half8(in ? ld16(x) : zero), x2 = as_half8(in ? ld16(x + half) : zero);
@@ -205,33 +215,35 @@ qknorm_dw_sum_kernel(const float* __restrict__ part, int nparts, int D, lt_half*
   }
 }
 
-// calls f with the lanes per head row as a constant: D / 16 rounded up to a power of two
+// calls f with the lanes per head row as a constant
 template <class F>
 hipError_t with_lanes(int D, F f) {
-  const int n = D / 16;
-  if (n <= 1) return f(std::integral_constant<int, 1>{});
-  if (n <= 2) return f(std::integral_constant<int, 2>{});
-  if (n <= 4) return f(std::integral_constant<int, 4>{});
-  if (n <= 8) return f(std::integral_constant<int, 8>{});
+  const int n = qknorm_lanes(D);
+  if (n == 1) return f(std::integral_constant<int, 1>{});
+  if (n == 2) return f(std::integral_constant<int, 2>{});
+  if (n == 4) return f(std::integral_constant<int, 4>{});
+  if (n == 8) return f(std::integral_constant<int, 8>{});
   return f(std::integral_constant<int, 16>{});
 }
 
 }  // namespace
 
 hipError_t qknorm_fwd_launch(const QkNormArgs& a, lt_half* Y, int64_t ldy, float* RSTD, float eps, hipStream_t s) {
+  const HeadSplit hs = qknorm_split(a.T, a.Hq + a.Hkv, a.D);
   return with_lanes(a.D, [&](auto L) {
-    hipLaunchKernelGGL((qknorm_fwd_kernel<decltype(L)::value>), dim3((unsigned)((a.T + kWaves - 1) / kWaves)),
-                       dim3(64 * kWaves), 0, s, a, Y, ldy, RSTD, eps);
+    hipLaunchKernelGGL((qknorm_fwd_kernel<decltype(L)::value>), dim3((unsigned)qknorm_blocks(hs)), dim3(64 * kWaves),
+                       0, s, a, hs, Y, ldy, RSTD, eps);
     return hipGetLastError();
   });
 }
 
 hipError_t qknorm_bwd_launch(const QkNormArgs& a, const lt_half* dY, int64_t lddy, const float* RSTD, lt_half* dX,
                              int64_t lddx, lt_half* dWq, lt_half* dWk, float* part, hipStream_t s) {
-  const int nblk = qknorm_bwd_blocks(a.T);
+  const int nblk = qknorm_bwd_blocks(a.T, a.Hq, a.Hkv, a.D);
+  const HeadSplit hq = qknorm_split(a.T, a.Hq, a.D), hk = qknorm_split(a.T, a.Hkv, a.D);
   const hipError_t e = with_lanes(a.D, [&](auto L) {
-    hipLaunchKernelGGL((qknorm_bwd_kernel<decltype(L)::value>), dim3((unsigned)nblk), dim3(64 * kWaves), 0, s, a, dY,
-                       lddy, RSTD, dX, lddx, part);
+    hipLaunchKernelGGL((qknorm_bwd_kernel<decltype(L)::value>), dim3((unsigned)nblk, nblk <= 256 ? 2 : 1),
+                       dim3(64 * kWaves), 0, s, a, hq, hk, dY, lddy, RSTD, dX, lddx, part);
     return hipGetLastError();
   });
   if (e != hipSuccess) return e;

@@ -75,7 +75,7 @@ hipError_t qknorm_bwd_launch(const QkNormArgs& a, const lt_half*, int64_t, const
                              lt_half*, float* part, hipStream_t) {
   ++g_launches;
   CHECK(a.POS || a.S <= a.P, "positions outside the table");
-  inside(part, (size_t)qknorm_bwd_blocks(a.T) * 2 * a.D * 4, 0, "dw partials");
+  inside(part, (size_t)qknorm_bwd_blocks(a.T, a.Hq, a.Hkv, a.D) * 2 * a.D * 4, 0, "dw partials");
   return hipErrorNoDevice;
 }
 hipError_t embed_fwd_launch(const int64_t*, const lt_half*, int64_t, float, lt_half*, int64_t, int64_t, int64_t,

@@ -50,6 +50,7 @@ CASES = [
     (255, 1000, 256, "zipf"), (256, 5000, 4096, "zipf"), (1000, 257, 520, "flat"), (1025, 32000, 1024, "zipf"),
     (3000, 2, 128, "two"), (2500, 700, 64, "one"), (4097, 300, 264, "zipf"), (777, 100, 8192, "two"),
     (50, 20, 64, "pads"), (20000, 3000, 48, "zipf"), (33, 70000, 64, "flat"),
+    (300, 40000, 8, "flat"), (20, 50000, 136, "zipf"), (9000, 600, 2568, "one"),
 ]
 
 

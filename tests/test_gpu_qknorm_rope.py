@@ -45,6 +45,11 @@ def rot_abs(a, c, s):
     (1, 50, 64, 8, 128, 64, 100.0, 0, False),
     (1, 513, 4, 4, 256, 32768, 1.0, 0, True),
     (1, 5001, 2, 1, 64, 5001, 1.0, 0, False),
+    # several tokens a wave, several waves a token
+    (1, 11, 1, 1, 128, 20, 1.0, 0, True),
+    (1, 3, 256, 32, 64, 8, 1.0, 0, False),
+    (1, 1, 9, 3, 112, 1, 1.0, 8, False),
+    (2, 550, 33, 11, 160, 600, 1.0, 0, False),
 ])
 @pytest.mark.parametrize("given", [True, False], ids=["positions", "in order"])
 def test_parity(env, B, S, Hq, Hkv, D, P, std, pad, inplace, given):
