@@ -374,6 +374,42 @@ def test_non_finite_value_reaches_those_who_see_it(env):
     check(got, clean, H_, 0.1, mask, 0.0, None)
 
 
+@pytest.mark.parametrize("S,Hq,Hkv,D,cap,biased", [(333, 6, 2, 64, 0.0, True), (700, 8, 8, 128, 30.0, False)])
+def test_separate_buffers(env, S, Hq, Hkv, D, cap, biased):
+    """Q, K, V, O and the gradients in buffers of their own, every row stride different: the same bits as
+    in the fused buffers.  One of the slopes is zero."""
+    torch, lt = env
+    rng, x = inputs(5 + S, 2, S, Hq, Hkv, D)
+    mask = make_mask("prefix", 2, S, rng)
+    slopes = slopes_of(Hq) if biased else None
+    if biased:
+        slopes[1] = 0.0
+    want = run_gpu(env, x, Hkv, D, 0.11, mask, cap, slopes)
+    check(want, x, Hkv, 0.11, mask, cap, slopes, {(1, Hkv - 1)})
+
+    def rows(a, pad):
+        t = torch.full((2 * S, a.shape[2] * D + pad), float("nan"), dtype=torch.float16, device="cuda")
+        t[:, :a.shape[2] * D] = torch.from_numpy(a.reshape(2 * S, -1)).cuda()
+        return t
+    up = lambda a: None if a is None else torch.from_numpy(a).cuda()
+    lo, hi, sl = up(mask[0]), up(mask[1]), up(slopes)
+    Q, K, V, dO = rows(x["Q"], 8), rows(x["K"], 24), rows(x["V"], 24), rows(x["dO"], 40)
+    O, dQ, dK, dV = torch.empty_like(dO), rows(0 * x["Q"], 56), rows(0 * x["K"], 72), rows(0 * x["V"], 72)
+    LSE = torch.empty(2, Hq, S, device="cuda")
+    lt.lt_attn_mod_fwd(Q, K, V, Q.stride(0), K.stride(0), O, O.stride(0), LSE, lo, hi, sl, cap, 2, S, Hq, Hkv, D, 0.11,
+                       mask[2])
+    n = lt.lt_attn_mod_bwd_workspace_size(2, S, Hq, Hkv, D, mask[2])
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    lt.lt_attn_mod_bwd(Q, K, V, Q.stride(0), K.stride(0), O, dO, O.stride(0), LSE, lo, hi, sl, cap, dQ, dK, dV,
+                       dQ.stride(0), dK.stride(0), ws, n, 2, S, Hq, Hkv, D, 0.11, mask[2])
+    for name, t, h in (("O", O, Hq), ("dQ", dQ, Hq), ("dK", dK, Hkv), ("dV", dV, Hkv)):
+        got = t[:, :h * D].cpu().numpy()
+        assert np.array_equal(got.view(np.uint16), want[name].reshape(2 * S, -1).view(np.uint16)), name
+        if name != "O":
+            assert bool(torch.isnan(t[:, h * D:]).all()), name
+    assert np.array_equal(LSE.cpu().numpy(), want["LSE"])
+
+
 @pytest.mark.parametrize("kind,cap,std", [("window", 50.0, 3.0), ("causal", 0.0, 3.0)])
 def test_gradients_of_concentrated_softmax(env, kind, cap, std):
     """Scores of deviation 9, so that rows rest on a few keys and dP - D cancels.  dQ and dK carry two
