@@ -7,8 +7,9 @@
 //
 //   * one workgroup = 4 waves = one (batch, query head, 128-query tile), or 64
 //     queries when 128-query tiles would fill at most one round of the CUs' two
-//     workgroup slots: then the two waves of a query group take one 32-key
-//     block of each slice each and merge their states through LDS;
+//     workgroup slots, and in a last round that is at most half full: then the two waves
+//     of a query group take one 32-key block of each slice each and merge their
+//     states through LDS;
 //   * S^T = K Q^T with 32x32x16 MFMA, so that a lane owns one query and its
 //     interval sits in two registers.  The workgroup walks the 64-key slices of
 //     the hull of its queries' intervals, last slice first (under a causal mask the
@@ -51,12 +52,13 @@ struct FwdSmem {
   static constexpr int STAGE = 2 * TILE;          // K then V
 };
 
+// Query tile qt (of 128 queries, or 64 with QSPLIT = 2) of (batch, head) bh.
 template <int D, int QSPLIT, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(NW * 64, 2)
-attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K, const lt_half* __restrict__ V,
-                    int64_t q_stride, int64_t kv_stride, lt_half* __restrict__ O, int64_t o_stride,
-                    float* __restrict__ LSE, const ScoreMod mod, int B, int S, int Hq, int Hkv, float scale,
-                    int causal) {
+__device__ __forceinline__ void
+fwd_tile(const lt_half* __restrict__ Q, const lt_half* __restrict__ K, const lt_half* __restrict__ V,
+         int64_t q_stride, int64_t kv_stride, lt_half* __restrict__ O, int64_t o_stride, float* __restrict__ LSE,
+         const ScoreMod& mod, int B, int S, int Hq, int Hkv, float scale, int causal, int qt, unsigned bh,
+         char* smem, int (*hull_s)[NW]) {
   using SM = FwdSmem<D>;
   using RT = RowTile<D, NW>;
   constexpr int KB = BKV / 32;     // 32-key blocks per slice
@@ -66,8 +68,6 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
   constexpr int BQW = NQG * 32;                    // queries per workgroup
   constexpr int KBW = KB / QSPLIT;                 // 32-key blocks per slice and wave
   static_assert(QSPLIT == 1 || NQG * DB * 4 * 64 * 16 + NQG * 64 * 8 <= 2 * SM::STAGE, "merge fits in LDS");
-  __shared__ __attribute__((aligned(1024))) char smem[2 * SM::STAGE];
-  __shared__ int hull_s[2][NW];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -77,10 +77,8 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
   const int qg = wave % NQG;                       // query group
   const int kpart = wave / NQG;                    // which block of each slice (QSPLIT = 2)
 
-  const int n_qt = (S + BQW - 1) / BQW;
-  const int qt = n_qt - 1 - (int)(blockIdx.x / (B * Hq));   // later queries mostly see more keys: longest first
   int b, h;
-  query_head(blockIdx.x % (B * Hq), B, Hq, Hkv, b, h);
+  query_head(bh, B, Hq, Hkv, b, h);
   const int kvh = h / (Hq / Hkv);
   const int q0 = qt * BQW;
   const int qw0 = q0 + qg * 32;
@@ -355,22 +353,46 @@ attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K
   }
 }
 
+// Workgroups 0 .. n_head - 1: 128 queries each, the last ones of every head first (later
+// queries mostly see more keys: longest first); the others 64 each.
+template <int D, bool HEAD, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(NW * 64, 2)
+attn_mod_fwd_kernel(const lt_half* __restrict__ Q, const lt_half* __restrict__ K, const lt_half* __restrict__ V,
+                    int64_t q_stride, int64_t kv_stride, lt_half* __restrict__ O, int64_t o_stride,
+                    float* __restrict__ LSE, const ScoreMod mod, int B, int S, int Hq, int Hkv, float scale,
+                    int causal, unsigned n_head) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * FwdSmem<D>::STAGE];
+  __shared__ int hull_s[2][NW];
+  const unsigned heads = B * Hq, bh = blockIdx.x % heads;
+  const int row = blockIdx.x / heads;
+  if (HEAD && blockIdx.x < n_head)
+    return fwd_tile<D, 1, CAP, BIAS>(Q, K, V, q_stride, kv_stride, O, o_stride, LSE, mod, B, S, Hq, Hkv, scale,
+                                     causal, (S + BQ - 1) / BQ - 1 - row, bh, smem, hull_s);
+  fwd_tile<D, 2, CAP, BIAS>(Q, K, V, q_stride, kv_stride, O, o_stride, LSE, mod, B, S, Hq, Hkv, scale, causal,
+                            (int)(gridDim.x / heads) - 1 - row, bh, smem, hull_s);
+}
+
 template <int D, bool CAP, bool BIAS>
 hipError_t launch_fwd(const AttnModFwdArgs& a, hipStream_t s) {
   const AttnShape& sh = a.sh;
-  // 64-query workgroups when 128-query ones would fill at most one round of
-  // the slots (short sequences)
-  const int64_t wgs128 = (int64_t)((sh.S + BQ - 1) / BQ) * sh.B * sh.Hq;
-  if (wgs128 > kFwdSlots) {
-    hipLaunchKernelGGL((attn_mod_fwd_kernel<D, 1, CAP, BIAS>), dim3((unsigned)wgs128), dim3(NW * 64), 0, s, a.Q,
-                       a.K, a.V, a.q_stride, a.kv_stride, a.O, a.o_stride, a.LSE, a.mod, sh.B, sh.S, sh.Hq,
-                       sh.Hkv, sh.scale, sh.causal);
-  } else {
-    const dim3 grid((unsigned)((int64_t)((sh.S + BQ / 2 - 1) / (BQ / 2)) * sh.B * sh.Hq));
-    hipLaunchKernelGGL((attn_mod_fwd_kernel<D, 2, CAP, BIAS>), grid, dim3(NW * 64), 0, s, a.Q, a.K, a.V,
+  // 64-query workgroups where 128-query ones would fill at most one round of the
+  // slots (short sequences), and for the rows of tiles of a last round that is at most half
+  // full: 2048 tokens of 40 heads, 640 workgroups, window of 683 and cap: 53.5 us against 60.1, with
+  // 64 queries throughout 65; 8 x 1024 tokens of 10 heads, full: 53.9 against 56.3; level or a
+  // little better in 16 other shapes of 576 to 4096 workgroups
+  const int64_t heads = (int64_t)sh.B * sh.Hq, rows = (sh.S + BQ - 1) / BQ, wgs = rows * heads;
+  const int64_t last = (wgs % kFwdSlots + heads - 1) / heads;
+  const int64_t head = wgs <= kFwdSlots ? 0 : last * heads <= kFwdSlots / 2 ? rows - last : rows;
+  const int64_t tail = head == 0 ? (sh.S + BQ / 2 - 1) / (BQ / 2) : 2 * (rows - head);
+  const dim3 grid((unsigned)((head + tail) * heads));
+  if (head > 0)
+    hipLaunchKernelGGL((attn_mod_fwd_kernel<D, true, CAP, BIAS>), grid, dim3(NW * 64), 0, s, a.Q, a.K, a.V, a.q_stride,
+                       a.kv_stride, a.O, a.o_stride, a.LSE, a.mod, sh.B, sh.S, sh.Hq, sh.Hkv, sh.scale, sh.causal,
+                       (unsigned)(head * heads));
+  else
+    hipLaunchKernelGGL((attn_mod_fwd_kernel<D, false, CAP, BIAS>), grid, dim3(NW * 64), 0, s, a.Q, a.K, a.V,
                        a.q_stride, a.kv_stride, a.O, a.o_stride, a.LSE, a.mod, sh.B, sh.S, sh.Hq, sh.Hkv, sh.scale,
-                       sh.causal);
-  }
+                       sh.causal, 0u);
   return hipGetLastError();
 }
 

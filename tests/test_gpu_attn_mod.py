@@ -253,6 +253,18 @@ def test_parity_of_drawn_shapes(env, seed):
     check(got, x, Hkv, 0.1, mask, cap, slopes)
 
 
+@pytest.mark.parametrize("B,S,Hq,Hkv,D,kind,cap,biased,std", [
+    (2, 700, 48, 16, 64, "prefix", 30.0, True, 2.0), (1, 1400, 56, 8, 128, "window", 0.0, False, 1.0),
+    (1, 1400, 56, 8, 128, "causal", 20.0, False, 1.0)])
+def test_tiles_of_two_sizes(env, B, S, Hq, Hkv, D, kind, cap, biased, std):
+    """More than 512 workgroups of 128 queries, the last few of them in halves: 2 x 48 heads of 6 tiles, 56 of 11."""
+    print("two sizes", B, S, Hq, Hkv, D, kind, cap, biased, std, flush=True)
+    rng, x = inputs(500 + S, B, S, Hq, Hkv, D, std)
+    mask, slopes = make_mask(kind, B, S, rng), slopes_of(Hq) if biased else None
+    got = run_gpu(env, x, Hkv, D, 1 / math.sqrt(D), mask, cap, slopes)
+    check(got, x, Hkv, 1 / math.sqrt(D), mask, cap, slopes, {(0, 0), (B - 1, Hkv - 1)})
+
+
 def test_every_key_hidden(env):
     """No query sees anything: zeros, -inf, and nothing read from the scores."""
     rng, x = inputs(7, 2, 100, 2, 2, 64)
