@@ -362,7 +362,7 @@ def test_non_finite_document_stays_to_itself(env, B, S, Hq, Hkv, D, cap, biased,
     x["Q"][:, first:last, :, 0] = np.nan
     got = run_gpu(env, x, Hkv, D, 0.1, mask, cap, slopes)
     assert np.isnan(got["O"][:, first:last].astype(np.float32)).all(-1).all()
-    for name in got:                                 # judge the other documents
+    for name in got:                                 # compare the other documents
         if name == "LSE":
             got[name][:, :, first:last] = want[name][:, :, first:last]
         else:
